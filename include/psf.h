@@ -348,6 +348,133 @@ psf_status psf_decode_prefill(const psf_desc *desc, const void *K, const void *V
                               size_t workspace_bytes, void *hip_stream);
 
 /*
+ * psf_layer_norm_fwd -- layer normalisation of rows, the step the paper puts before the attention kernel (Section
+ * 2.1; Q and K rows there, a model's tokens elsewhere): with mean m and deviation s = sqrt(var + eps) of a
+ * row (biased variance), y = (x - m) / s * weight + bias.
+ *   x, y [rows, width], weight, bias [width]: device, dtype (psf_dtype); bias may be NULL; y may be x.
+ *   stats: fp32 [rows, 2] (m, 1 / s), device, 8-byte aligned, written for the backward call; NULL to skip it.
+ * 1 <= width <= PSF_NORM_MAX_WIDTH, 1 <= rows < 2^31, eps > 0; the tensors need the alignment of their
+ * type only (PSF_ERR_ALIGNMENT).  Statistics and sums are fp32.
+ *
+ * psf_layer_norm_bwd -- its gradients: dx [rows, width], dweight, dbias [width] (dbias may be NULL), each written
+ * once, in dtype; stats as the forward call left them; dx may be dy.  The sums over rows are fp32 in a fixed
+ * order (no atomics: a repeated call returns the same bits).
+ *   workspace: psf_layer_norm_bwd_workspace_bytes(rows, width, dtype) bytes, 256-byte aligned.
+ */
+#define PSF_NORM_MAX_WIDTH 8192
+psf_status psf_layer_norm_fwd(int64_t rows, int32_t width, int32_t dtype, float eps, const void *x, const void *weight,
+                              const void *bias, void *y, float *stats, void *hip_stream);
+size_t psf_layer_norm_bwd_workspace_bytes(int64_t rows, int32_t width, int32_t dtype);
+psf_status psf_layer_norm_bwd(int64_t rows, int32_t width, int32_t dtype, const void *x, const void *weight,
+                              const float *stats, const void *dy, void *dx, void *dweight, void *dbias, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Softmax attention with a sliding window, for the layers that stand beside the sketched ones: row i sees key j
+ * if j <= i and (i - j < window or j < sinks) -- its last `window` tokens, itself among them, and
+ * the first `sinks` tokens of the sequence --, and o_i = sum_j softmax_j(scale <q_i, k_j>) v_j.
+ * window >= n is plain causal attention.
+ */
+typedef enum { PSF_HEADS_FIRST = 0,      /* Q, O [batch, heads, n, d], K, V [batch, kv_heads, n, d]   */
+               PSF_TOKENS_FIRST = 1 } psf_layout;   /* [batch, n, heads | kv_heads, d]                */
+#define PSF_WINDOW_MAX_DIM 128
+typedef struct {
+    int32_t batch, heads;
+    int32_t kv_heads;        /* heads % kv_heads == 0; query head h reads key head h / (heads / kv_heads) */
+    int32_t n, d;            /* tokens, row length (a multiple of 8, at most PSF_WINDOW_MAX_DIM)      */
+    int32_t window, sinks;   /* window >= 1, sinks >= 0                                               */
+    int32_t dtype;           /* psf_dtype of every tensor                                             */
+    int32_t layout;          /* psf_layout of every tensor                                            */
+    float scale;             /* of the scores, 1 / sqrt(d) as a rule                                  */
+} psf_window_desc;
+psf_status psf_check_window_desc(const psf_window_desc *desc);
+
+/*
+ * psf_window_attn_fwd -- O as above.  lengths: int32 [batch] (device) or NULL (all n): sequence b has its first
+ * lengths[b] tokens (taken as 0 below 0, as n above n); rows behind them are not read, their
+ * results are zero.  lse: fp32 [batch, heads, n] (device), log of the sum of exponentials of every row for
+ * the backward call (-inf behind the length); NULL to skip it.  Tensors 16-byte aligned (PSF_ERR_ALIGNMENT).
+ * Sums are fp32; in bf16 storage the weights are rounded to bf16 for their product with V.
+ * An infinity or NaN of a token reaches no row that does not see the token.
+ *
+ * psf_window_attn_bwd -- gradients of L(O) for a given dO: dQ, dK, dV in the layout of Q, K, V, each written once
+ * (zero behind the lengths); O and lse as the forward call wrote them.  dK and dV are summed over the query
+ * heads that share the key head.  No atomics: a repeated call returns the same bits.  In bf16 storage
+ * weights and their gradients are rounded to bf16 for their products.  An infinity or NaN reaches no gradient of a
+ * token with which it shares no visible pair.
+ *   workspace: psf_window_attn_bwd_workspace_bytes(desc) bytes, 256-byte aligned.
+ * Nothing is allocated and nothing synchronises.
+ */
+psf_status psf_window_attn_fwd(const psf_window_desc *desc, const void *Q, const void *K, const void *V, const int32_t *lengths,
+                               void *O, float *lse, void *hip_stream);
+size_t psf_window_attn_bwd_workspace_bytes(const psf_window_desc *desc);
+psf_status psf_window_attn_bwd(const psf_window_desc *desc, const void *Q, const void *K, const void *V, const int32_t *lengths,
+                               const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
+/*
+ * A paged key-value cache for the window layers (the sketched ones keep the state of psf_decode_step).  The caller
+ * owns two pools Kp, Vp [pages, kv_heads, page, d], 16-byte aligned; row s of the block table
+ * [seqs, cols] (int32) names the pages of sequence s in order: position t of the sequence is slot t % page of
+ * page table[s][t / page].  lengths: int32 [seqs].  An entry outside [0, pages) -- -1 by custom -- stands for no
+ * page: nothing is written there, and its positions are not visible.  Tables, lengths and every list of sequences or pages
+ * are device memory; they are read and checked on the device, so that no content of them leads
+ * outside the pools, but a list that names a place twice (or a page that two sequences write) leaves
+ * unspecified which content that place gets.
+ */
+#define PSF_CACHE_MAX_DIM 128
+#define PSF_CACHE_MAX_PAGES (1 << 20)
+typedef struct {
+    int32_t pages, page;     /* pages of the pools, tokens of a page                                  */
+    int32_t kv_heads, d;     /* d a multiple of 8, at most PSF_CACHE_MAX_DIM                          */
+    int32_t seqs, cols;      /* rows and columns of the block table                                   */
+    int32_t dtype;           /* psf_dtype of the pools                                                */
+} psf_cache_desc;            /* pages * page * kv_heads, seqs * cols and cols * page below 2^31       */
+psf_status psf_check_cache_desc(const psf_cache_desc *desc);
+
+/*
+ * psf_cache_append -- token t < counts[s] of K, V [seqs, kv_heads, n, d] goes to position lengths[s] + t of sequence
+ * s (counts: int32 [seqs], at most n each; NULL: n everywhere).  lengths are those before the call and stay as
+ * they are; positions behind the table are left out, and so are sequences with a negative length.
+ */
+psf_status psf_cache_append(const psf_cache_desc *desc, int32_t n, const void *K, const void *V, void *Kp, void *Vp,
+                            const int32_t *table, const int32_t *lengths, const int32_t *counts, void *hip_stream);
+
+/*
+ * psf_cache_fork -- for k < forks: sequence children[k] becomes what parents[k] is.  It shares the parent's pages, but
+ * for a last page that is not full, whose content is copied to page fresh[k] (not read otherwise); row children[k] of
+ * the table and lengths[children[k]] are overwritten.  A parent of several children is fine; a child that is
+ * also a parent in the same call, or named twice, gets unspecified content.  Pairs with a sequence outside
+ * [0, seqs), or with parent == child, are left out.
+ */
+psf_status psf_cache_fork(const psf_cache_desc *desc, int32_t forks, void *Kp, void *Vp, int32_t *table, int32_t *lengths,
+                          const int32_t *parents, const int32_t *children, const int32_t *fresh, void *hip_stream);
+
+/*
+ * psf_cache_compact -- brings the pages in use to the front of the pools.  In use are the pages of the table's first
+ * ceil(lengths[s] / page) columns of every row; with `live` of them, the k-th page below `live` that is not in use takes the
+ * content of the k-th page from `live` on that is (both in ascending order), and new_table [seqs, cols] is the
+ * table with the new places, -1 behind the lengths and where the table names no page.  Afterwards the pages from *live
+ * on are free.  new_table must not be table (which stays valid for the pages that did not move).
+ *   live: int32 [1] (device).  workspace: psf_cache_compact_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+size_t psf_cache_compact_workspace_bytes(const psf_cache_desc *desc);
+psf_status psf_cache_compact(const psf_cache_desc *desc, void *Kp, void *Vp, const int32_t *table, const int32_t *lengths,
+                             int32_t *new_table, int32_t *live, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * psf_paged_attn -- the last row of psf_window_attn_fwd for every sequence of the cache: q [seqs, heads, 1, d] is the
+ * query of position lengths[s] - 1 (whose key and value are in the cache already), o [seqs, heads, 1, d] its result;
+ * a sequence without visible positions gets zeros.  window >= 1 (INT32_MAX: all positions), sinks >= 0, scale as above.
+ * Pages none of whose positions are visible are not read and may be absent (freed).
+ *   workspace: psf_paged_workspace_bytes(desc, heads) bytes, 256-byte aligned (NULL where that is 0).
+ */
+size_t psf_paged_workspace_bytes(const psf_cache_desc *desc, int32_t heads);
+psf_status psf_paged_attn(const psf_cache_desc *desc, int32_t heads, int32_t window, int32_t sinks, float scale, const void *q,
+                          const void *Kp, const void *Vp, const int32_t *table, const int32_t *lengths, void *o,
+                          void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Measurement aid (not part of the attention path): launches `workgroups` workgroups of four
  * wavefronts, each wavefront issuing iters x 8 independent v_mfma_f32_32x32x16_bf16 on non-zero
  * operands, i.e. workgroups x 4 x iters x 8 x 32768 flops in all.  A benchmark times it with

@@ -7,6 +7,7 @@ sketch matrices G are constants of the layer (Algorithm 1 draws them once): they
 gradient.  With learned sketches (Algorithm 2) G holds the networks' parameters, which are
 trained with the model: when G requires a gradient the backward is
 psf_causal_attn_bwd_saved_learned / psf_causal_attn_bwd_learned and G receives the parameter gradient (accumulated in fp32 by the library, returned in G's dtype).
+layer_norm and causal_window_attention are the differentiable forms of psf_layer_norm_* and psf_window_attn_*.
 """
 import torch
 
@@ -58,3 +59,58 @@ def causal_polysketch_attention(Q, K, V, G, p, r, b, local=psf.LOCAL_EXACT, per_
     desc = psf.make_desc(B, H, n, d, p, r, b, dtype, dv=V.shape[-1], local=local, per_head=per_head,
                          learned=learned)
     return _CausalPolysketchAttention.apply(Q, K, V, G, desc)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        x = x.contiguous()
+        y, stats = psf.psf_layer_norm_fwd(x, weight, bias, eps, want_stats=True)
+        ctx.save_for_backward(x, weight, stats)
+        ctx.has_bias = bias is not None
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, stats = ctx.saved_tensors
+        dx, dweight, dbias = psf.psf_layer_norm_bwd(x, weight, stats, dy.contiguous(), want_bias=ctx.has_bias)
+        return dx, dweight, dbias, None
+
+
+def layer_norm(x, weight, bias=None, eps=1e-6):
+    """Differentiable layer normalisation over the last axis of x (at most 8192 long), float32 or bfloat16: the step the
+    paper puts before the attention (Section 2.1), for Q and K rows or a model's tokens.  weight and
+    bias [width] in x's dtype."""
+    return _LayerNorm.apply(x, weight.contiguous(), None if bias is None else bias.contiguous(), eps)
+
+
+class _CausalWindowAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, Q, K, V, lengths, desc):
+        Q, K, V = Q.contiguous(), K.contiguous(), V.contiguous()
+        O, lse = psf.psf_window_attn_fwd(desc, Q, K, V, lengths=lengths, want_lse=True)
+        ctx.desc = desc
+        ctx.save_for_backward(Q, K, V, lengths, O, lse)
+        return O
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dO):
+        Q, K, V, lengths, O, lse = ctx.saved_tensors
+        dQ, dK, dV = psf.psf_window_attn_bwd(ctx.desc, Q, K, V, O, lse, dO.contiguous(), lengths=lengths)
+        return dQ, dK, dV, None, None
+
+
+def causal_window_attention(Q, K, V, window=None, sinks=0, lengths=None, scale=None, tokens_first=False):
+    """Differentiable softmax attention in which row i sees its last `window` tokens (None: all) and the first `sinks`
+    tokens of the sequence.  Q [batch, heads, n, d], K and V [batch, kv_heads, n, d], heads a multiple of kv_heads,
+    or with tokens_first all of them [batch, n, heads, d]; d a multiple of 8, at most 128.  lengths: int32 [batch] on the
+    GPU, tokens of each sequence (rows behind them give zeros and get zero gradients)."""
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("Q, K, V must have four axes")
+    at = 2 if tokens_first else 1
+    dtype = {torch.float32: "f32", torch.bfloat16: "bf16"}[Q.dtype]
+    desc = psf.make_window_desc(Q.shape[0], Q.shape[at], Q.shape[3 - at], Q.shape[3], window, sinks, dtype,
+                                kv_heads=K.shape[at], tokens_first=tokens_first, scale=scale)
+    return _CausalWindowAttention.apply(Q, K, V, lengths, desc)

@@ -4,6 +4,7 @@ torch supplies device memory and the stream; every step of the path runs inside 
 library's HIP kernels.  There is no CPU fallback: a missing library or a CPU tensor
 raises.
 """
+import contextlib
 import ctypes
 import functools
 import os
@@ -26,13 +27,26 @@ EXPORTS = ("psf_check_desc", "psf_kernel_path", "psf_fwd_beside_states", "psf_ge
            "psf_causal_attn_bwd_saved", "psf_causal_attn_bwd_saved_learned", "psf_bwd_kernel_path", "psf_bwd_workspace_bytes", "psf_causal_attn_bwd",
            "psf_causal_attn_bwd_learned",
            "psf_causal_attn_bwd_timed", "psf_decode_state_bytes", "psf_decode_reset",
-           "psf_decode_step", "psf_decode_prefill_workspace_bytes", "psf_decode_prefill", "psf_probe_mfma_loop")
+           "psf_decode_step", "psf_decode_prefill_workspace_bytes", "psf_decode_prefill", "psf_probe_mfma_loop",
+           "psf_layer_norm_fwd", "psf_layer_norm_bwd_workspace_bytes", "psf_layer_norm_bwd",
+           "psf_check_window_desc", "psf_window_attn_fwd", "psf_window_attn_bwd_workspace_bytes", "psf_window_attn_bwd",
+           "psf_check_cache_desc", "psf_cache_append", "psf_cache_fork", "psf_cache_compact_workspace_bytes",
+           "psf_cache_compact", "psf_paged_workspace_bytes", "psf_paged_attn")
 
 
 class PsfDesc(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in
                 ("batch", "heads", "n", "d", "dv", "p", "r", "b", "dtype", "feat", "local",
                  "sketch_per_head", "learned")]
+
+
+class PsfWindowDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("batch", "heads", "kv_heads", "n", "d", "window", "sinks", "dtype", "layout")] + [("scale", ctypes.c_float)]
+
+
+class PsfCacheDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("pages", "page", "kv_heads", "d", "seqs", "cols", "dtype")]
 
 
 class PsfError(RuntimeError):
@@ -118,6 +132,24 @@ def lib():
         L.psf_decode_prefill.argtypes = [dp, vp, vp, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp]
         L.psf_probe_mfma_loop.restype = ctypes.c_int
         L.psf_probe_mfma_loop.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp]
+        i32, i64, f32, size, wp, cp = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t,
+                                       ctypes.POINTER(PsfWindowDesc), ctypes.POINTER(PsfCacheDesc))
+        for name, restype, argtypes in (
+                ("psf_layer_norm_fwd", ctypes.c_int, [i64, i32, i32, f32] + [vp] * 6),
+                ("psf_layer_norm_bwd_workspace_bytes", size, [i64, i32, i32]),
+                ("psf_layer_norm_bwd", ctypes.c_int, [i64, i32, i32] + [vp] * 8 + [size, vp]),
+                ("psf_check_window_desc", ctypes.c_int, [wp]),
+                ("psf_window_attn_fwd", ctypes.c_int, [wp] + [vp] * 7),
+                ("psf_window_attn_bwd_workspace_bytes", size, [wp]),
+                ("psf_window_attn_bwd", ctypes.c_int, [wp] + [vp] * 11 + [size, vp]),
+                ("psf_check_cache_desc", ctypes.c_int, [cp]),
+                ("psf_cache_append", ctypes.c_int, [cp, i32] + [vp] * 8),
+                ("psf_cache_fork", ctypes.c_int, [cp, i32] + [vp] * 8),
+                ("psf_cache_compact_workspace_bytes", size, [cp]),
+                ("psf_cache_compact", ctypes.c_int, [cp] + [vp] * 7 + [size, vp]),
+                ("psf_paged_workspace_bytes", size, [cp, i32]),
+                ("psf_paged_attn", ctypes.c_int, [cp, i32, i32, i32, f32] + [vp] * 7 + [size, vp])):
+            getattr(L, name).restype, getattr(L, name).argtypes = restype, argtypes
         L.psf_stage_name.restype = ctypes.c_char_p
         L.psf_stage_name.argtypes = [ctypes.c_int, ctypes.c_int32]
         L.psf_status_string.restype = ctypes.c_char_p
@@ -512,6 +544,273 @@ def psf_decode_step(desc, q, k, v, G, pos, state, o=None, stream=None):
         _dev_ptr(o, desc, (B, H, 1, dv), "o"), _stream_ptr(stream))
     if st != PSF_OK:
         raise PsfError(st, "psf_decode_step")
+    return o
+
+
+# ---- layer normalisation, window attention, paged cache ------------------------------------------
+# These calls run on the device of their tensors and on `stream` (default: that device's current one); what
+# they allocate themselves is allocated for that stream.
+
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+EVERYTHING = 2 ** 31 - 1             # a window that hides nothing
+
+
+def _place(tensors, stream):
+    """(context, device) of a call on these GPU tensors: with the context the device is the current one and `stream`
+    the current stream."""
+    device = None
+    for name, t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("%s must live on the GPU (no CPU path exists)" % name)
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("%s lives on %s, the call's other tensors on %s" % (name, t.device, device))
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError("the stream belongs to %s, the tensors live on %s" % (stream.device, device))
+        return torch.cuda.stream(stream), device
+    if device.index != torch._C._cuda_getDevice():
+        return torch.cuda.device(device), device
+    return contextlib.nullcontext(), device
+
+
+def _ptr(t, dtype, shape, name):
+    """Address of a contiguous tensor of this type and shape (None: no tensor)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return t.data_ptr()
+
+
+def _room(workspace, nbytes, device, name="workspace"):
+    """The caller's workspace, or one allocated for the current stream (None where nothing is needed)."""
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    if not workspace.is_cuda or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("%s must be a contiguous uint8 GPU tensor" % name)
+    if workspace.device != device:
+        raise ValueError("%s lives on %s, the call's other tensors on %s" % (name, workspace.device, device))
+    return workspace
+
+
+def _room_args(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+
+
+def _done(st, where):
+    if st != PSF_OK:
+        raise PsfError(st, where)
+
+
+def _norm_rows(x):
+    if x.dim() == 0 or x.dtype not in _CODES:
+        raise ValueError("x must be a float32 or bfloat16 tensor of rows")
+    width = x.shape[-1]
+    return (x.numel() // width if width else 0), width
+
+
+def psf_layer_norm_fwd(x, weight, bias=None, eps=1e-6, y=None, stats=None, want_stats=False, stream=None):
+    """Layer normalisation over the last axis; returns y, or (y, stats) with want_stats or a stats tensor ([rows, 2]
+    fp32: mean and inverse deviation, for psf_layer_norm_bwd)."""
+    rows, width = _norm_rows(x)
+    where, device = _place((("x", x), ("weight", weight), ("bias", bias), ("y", y), ("stats", stats)), stream)
+    with where:
+        if y is None:
+            y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        if stats is None and want_stats:
+            stats = torch.empty(rows, 2, dtype=torch.float32, device=device)
+        _done(lib().psf_layer_norm_fwd(rows, width, _CODES[x.dtype], eps, _ptr(x, x.dtype, None, "x"),
+                                       _ptr(weight, x.dtype, (width,), "weight"), _ptr(bias, x.dtype, (width,), "bias"),
+                                       _ptr(y, x.dtype, x.shape, "y"), _ptr(stats, torch.float32, (rows, 2), "stats"),
+                                       _stream_ptr(None)), "psf_layer_norm_fwd")
+    return y if stats is None else (y, stats)
+
+
+def psf_layer_norm_bwd(x, weight, stats, dy, want_bias=True, workspace=None, stream=None):
+    """Gradients of psf_layer_norm_fwd: (dx, dweight, dbias), dbias None without want_bias."""
+    rows, width = _norm_rows(x)
+    where, device = _place((("x", x), ("weight", weight), ("stats", stats), ("dy", dy)), stream)
+    with where:
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        dweight = torch.empty_like(weight)
+        dbias = torch.empty_like(weight) if want_bias else None
+        code = _CODES[x.dtype]
+        workspace = _room(workspace, lib().psf_layer_norm_bwd_workspace_bytes(rows, width, code), device)
+        _done(lib().psf_layer_norm_bwd(rows, width, code, _ptr(x, x.dtype, None, "x"), _ptr(weight, x.dtype, (width,), "weight"),
+                                       _ptr(stats, torch.float32, (rows, 2), "stats"), _ptr(dy, x.dtype, x.shape, "dy"),
+                                       dx.data_ptr(), dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                                       *_room_args(workspace), _stream_ptr(None)), "psf_layer_norm_bwd")
+    return dx, dweight, dbias
+
+
+def make_window_desc(batch, heads, n, d, window=None, sinks=0, dtype="bf16", kv_heads=None, tokens_first=False, scale=None):
+    """window None: every earlier token (plain causal attention); scale None: 1 / sqrt(d)."""
+    code = {"f32": F32, "bf16": BF16}[dtype] if isinstance(dtype, str) else int(dtype)
+    return PsfWindowDesc(batch, heads, heads if kv_heads is None else kv_heads, n, d, EVERYTHING if window is None else window,
+                         sinks, code, int(bool(tokens_first)), d ** -0.5 if scale is None else scale)
+
+
+def check_window_desc(desc):
+    return lib().psf_check_window_desc(ctypes.byref(desc))
+
+
+def _window_shapes(desc):
+    """Shapes of Q and of K."""
+    return tuple((desc.batch, desc.n, h, desc.d) if desc.layout else (desc.batch, h, desc.n, desc.d)
+                 for h in (desc.heads, desc.kv_heads))
+
+
+def psf_window_attn_fwd(desc, Q, K, V, lengths=None, O=None, lse=None, want_lse=False, stream=None):
+    """Causal attention with a sliding window; returns O, or (O, lse) with want_lse or an lse tensor ([batch, heads, n]
+    fp32, for psf_window_attn_bwd).  lengths: int32 [batch] on the GPU, or None."""
+    _done(check_window_desc(desc), "psf_window_attn_fwd")
+    shape_q, shape_k = _window_shapes(desc)
+    dtype, rows = _torch_dtype(desc), (desc.batch, desc.heads, desc.n)
+    where, device = _place((("Q", Q), ("K", K), ("V", V), ("lengths", lengths), ("O", O), ("lse", lse)), stream)
+    with where:
+        if O is None:
+            O = torch.empty(shape_q, dtype=dtype, device=device)
+        if lse is None and want_lse:
+            lse = torch.empty(rows, dtype=torch.float32, device=device)
+        _done(lib().psf_window_attn_fwd(
+            ctypes.byref(desc), _ptr(Q, dtype, shape_q, "Q"), _ptr(K, dtype, shape_k, "K"), _ptr(V, dtype, shape_k, "V"),
+            _ptr(lengths, torch.int32, (desc.batch,), "lengths"), _ptr(O, dtype, shape_q, "O"),
+            _ptr(lse, torch.float32, rows, "lse"), _stream_ptr(None)), "psf_window_attn_fwd")
+    return O if lse is None else (O, lse)
+
+
+def window_bwd_workspace_bytes(desc):
+    return lib().psf_window_attn_bwd_workspace_bytes(ctypes.byref(desc))
+
+
+def psf_window_attn_bwd(desc, Q, K, V, O, lse, dO, lengths=None, workspace=None, stream=None):
+    """Gradients of psf_window_attn_fwd; returns (dQ, dK, dV)."""
+    _done(check_window_desc(desc), "psf_window_attn_bwd")
+    shape_q, shape_k = _window_shapes(desc)
+    dtype = _torch_dtype(desc)
+    where, device = _place((("Q", Q), ("K", K), ("V", V), ("O", O), ("lse", lse), ("dO", dO), ("lengths", lengths)), stream)
+    with where:
+        workspace = _room(workspace, window_bwd_workspace_bytes(desc), device)
+        dQ, dK, dV = (torch.empty(shape, dtype=dtype, device=device) for shape in (shape_q, shape_k, shape_k))
+        _done(lib().psf_window_attn_bwd(
+            ctypes.byref(desc), _ptr(Q, dtype, shape_q, "Q"), _ptr(K, dtype, shape_k, "K"), _ptr(V, dtype, shape_k, "V"),
+            _ptr(lengths, torch.int32, (desc.batch,), "lengths"), _ptr(O, dtype, shape_q, "O"),
+            _ptr(lse, torch.float32, (desc.batch, desc.heads, desc.n), "lse"), _ptr(dO, dtype, shape_q, "dO"),
+            dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), *_room_args(workspace), _stream_ptr(None)), "psf_window_attn_bwd")
+    return dQ, dK, dV
+
+
+def make_cache_desc(pages, page, kv_heads, d, seqs, cols, dtype="bf16"):
+    """Pools of `pages` pages of `page` tokens, a block table of seqs rows and cols columns."""
+    code = {"f32": F32, "bf16": BF16}[dtype] if isinstance(dtype, str) else int(dtype)
+    return PsfCacheDesc(pages, page, kv_heads, d, seqs, cols, code)
+
+
+def check_cache_desc(desc):
+    return lib().psf_check_cache_desc(ctypes.byref(desc))
+
+
+def cache_new_pools(desc, device="cuda"):
+    """Kp, Vp [pages, kv_heads, page, d] (uninitialised)."""
+    _done(check_cache_desc(desc), "cache_new_pools")
+    return tuple(torch.empty(desc.pages, desc.kv_heads, desc.page, desc.d, dtype=_torch_dtype(desc), device=device)
+                 for _ in range(2))
+
+
+def _cache_ptrs(desc, Kp, Vp, table, lengths):
+    shape = (desc.pages, desc.kv_heads, desc.page, desc.d)
+    return (_ptr(Kp, _torch_dtype(desc), shape, "Kp"), _ptr(Vp, _torch_dtype(desc), shape, "Vp"),
+            _ptr(table, torch.int32, (desc.seqs, desc.cols), "table"), _ptr(lengths, torch.int32, (desc.seqs,), "lengths"))
+
+
+def psf_cache_append(desc, K, V, Kp, Vp, table, lengths, counts=None, stream=None):
+    """Tokens t < counts[s] of K, V [seqs, kv_heads, n, d] to positions lengths[s] + t of the cache (counts None: all n).
+    lengths are those before the call; the caller advances them."""
+    _done(check_cache_desc(desc), "psf_cache_append")
+    if K.dim() != 4:
+        raise ValueError("K must be [seqs, kv_heads, n, d]")
+    n, dtype = K.shape[2], _torch_dtype(desc)
+    shape = (desc.seqs, desc.kv_heads, n, desc.d)
+    where, _ = _place((("K", K), ("V", V), ("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("counts", counts)),
+                      stream)
+    with where:
+        _done(lib().psf_cache_append(ctypes.byref(desc), n, _ptr(K, dtype, shape, "K"), _ptr(V, dtype, shape, "V"),
+                                     *_cache_ptrs(desc, Kp, Vp, table, lengths),
+                                     _ptr(counts, torch.int32, (desc.seqs,), "counts"), _stream_ptr(None)), "psf_cache_append")
+
+
+def psf_cache_fork(desc, Kp, Vp, table, lengths, parents, children, fresh, stream=None):
+    """Sequence children[k] becomes a copy of parents[k] that shares its full pages; a last page that is not full is copied
+    to page fresh[k].  Writes the children's rows of table and lengths."""
+    _done(check_cache_desc(desc), "psf_cache_fork")
+    forks = (parents.numel(),)
+    where, _ = _place((("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("parents", parents),
+                       ("children", children), ("fresh", fresh)), stream)
+    with where:
+        _done(lib().psf_cache_fork(ctypes.byref(desc), forks[0], *_cache_ptrs(desc, Kp, Vp, table, lengths),
+                                   *(_ptr(t, torch.int32, forks, name) for t, name in
+                                     ((parents, "parents"), (children, "children"), (fresh, "fresh"))), _stream_ptr(None)),
+              "psf_cache_fork")
+
+
+def alloc_compact_workspace(desc, device="cuda"):
+    return torch.empty(max(lib().psf_cache_compact_workspace_bytes(ctypes.byref(desc)), 256), dtype=torch.uint8, device=device)
+
+
+def psf_cache_compact(desc, Kp, Vp, table, lengths, new_table=None, live=None, workspace=None, stream=None):
+    """Moves the pages in use to the front of the pools; returns (new_table, live): the table with the new places and the
+    number of pages in use (int32 [1] on the GPU; the pages from it on are free)."""
+    _done(check_cache_desc(desc), "psf_cache_compact")
+    where, device = _place((("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("new_table", new_table),
+                            ("live", live)), stream)
+    with where:
+        if new_table is None:
+            new_table = torch.empty_like(table)
+        elif new_table.data_ptr() == table.data_ptr():
+            raise ValueError("new_table must not be table")
+        if live is None:
+            live = torch.empty(1, dtype=torch.int32, device=device)
+        workspace = _room(workspace, lib().psf_cache_compact_workspace_bytes(ctypes.byref(desc)), device)
+        _done(lib().psf_cache_compact(ctypes.byref(desc), *_cache_ptrs(desc, Kp, Vp, table, lengths),
+                                      _ptr(new_table, torch.int32, (desc.seqs, desc.cols), "new_table"),
+                                      _ptr(live, torch.int32, (1,), "live"), *_room_args(workspace), _stream_ptr(None)),
+              "psf_cache_compact")
+    return new_table, live
+
+
+def paged_workspace_bytes(desc, heads):
+    return lib().psf_paged_workspace_bytes(ctypes.byref(desc), heads)
+
+
+def alloc_paged_workspace(desc, heads, device="cuda"):
+    return torch.empty(max(paged_workspace_bytes(desc, heads), 256), dtype=torch.uint8, device=device)
+
+
+def psf_paged_attn(desc, q, Kp, Vp, table, lengths, window=None, sinks=0, scale=None, o=None, workspace=None, stream=None):
+    """Attention of one new token a sequence (q [seqs, heads, 1, d], at position lengths - 1, its key and value in the
+    cache already) over the paged cache; returns o of q's shape.  window None: every position."""
+    _done(check_cache_desc(desc), "psf_paged_attn")
+    if q.dim() != 4:
+        raise ValueError("q must be [seqs, heads, 1, d]")
+    heads, dtype = q.shape[1], _torch_dtype(desc)
+    shape = (desc.seqs, heads, 1, desc.d)
+    where, device = _place((("q", q), ("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("o", o)), stream)
+    with where:
+        if o is None:
+            o = torch.empty(shape, dtype=dtype, device=device)
+        workspace = _room(workspace, paged_workspace_bytes(desc, heads), device)
+        _done(lib().psf_paged_attn(ctypes.byref(desc), heads, EVERYTHING if window is None else window, sinks,
+                                   desc.d ** -0.5 if scale is None else scale, _ptr(q, dtype, shape, "q"),
+                                   *_cache_ptrs(desc, Kp, Vp, table, lengths), _ptr(o, dtype, shape, "o"),
+                                   *_room_args(workspace), _stream_ptr(None)), "psf_paged_attn")
     return o
 
 

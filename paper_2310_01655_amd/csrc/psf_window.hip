@@ -1,0 +1,123 @@
+// Entry points of the window attention: the descriptor's check, the choice of kernels, D = <dO, O>.
+#include <initializer_list>
+#include "psf_window.h"
+
+namespace psf {
+namespace {
+
+psf_status make_window(const psf_window_desc *desc, Window *out)
+{
+    if (!desc) return PSF_ERR_NULL;
+    if (desc->batch <= 0 || desc->heads <= 0 || desc->kv_heads <= 0 || desc->n <= 0 || desc->d <= 0 || desc->window <= 0 ||
+        desc->sinks < 0 || desc->heads % desc->kv_heads != 0)
+        return PSF_ERR_SHAPE;
+    if (desc->dtype != PSF_F32 && desc->dtype != PSF_BF16) return PSF_ERR_UNSUPPORTED;
+    if (desc->layout != PSF_HEADS_FIRST && desc->layout != PSF_TOKENS_FIRST) return PSF_ERR_UNSUPPORTED;
+    if (desc->d % 8 != 0 || desc->d > PSF_WINDOW_MAX_DIM) return PSF_ERR_UNSUPPORTED;
+    // (batch, head) pairs index grid dimension y; positions plus a window stay inside 32 bits; a tile's rows
+    // lie within 4 GB of each other
+    if ((long long)desc->batch * desc->heads > 65535 || desc->n > (1 << 24) || (long long)desc->heads * desc->d > (1 << 20))
+        return PSF_ERR_UNSUPPORTED;
+    Window w;
+    w.batch = desc->batch; w.heads = desc->heads; w.kv_heads = desc->kv_heads; w.group = desc->heads / desc->kv_heads;
+    w.n = desc->n; w.d = desc->d;
+    w.window = desc->window < desc->n ? desc->window : desc->n;
+    w.sinks = desc->sinks < desc->n ? desc->sinks : desc->n;
+    w.bf16 = desc->dtype == PSF_BF16;
+    w.scale = desc->scale;
+    w.scale2 = desc->scale * kWindowLog2e;
+    const int64_t n = w.n, d = w.d;
+    const bool tokens = desc->layout == PSF_TOKENS_FIRST;
+    w.batch_q = n * w.heads * d;    w.head_q = tokens ? d : n * d; w.row_q = tokens ? w.heads * d : d;
+    w.batch_k = n * w.kv_heads * d; w.head_k = tokens ? d : n * d; w.row_k = tokens ? w.kv_heads * d : d;
+    *out = w;
+    return PSF_OK;
+}
+
+// D of every row: 16 lanes a row, 8 columns a lane.
+template <typename S>
+__global__ __launch_bounds__(256) void window_delta_kernel(const S *O, const S *dO, float *delta, Window w, int64_t rows)
+{
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int c = 8 * (threadIdx.x % 16);
+    float s = 0.f;
+    if (row < rows && c < w.d) {
+        const int64_t unit = row / w.n, i = row - unit * w.n, b = unit / w.heads, h = unit - b * w.heads;
+        const int64_t at = b * w.batch_q + h * w.head_q + i * w.row_q + c;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += load_f(O, at + k) * load_f(dO, at + k);
+    }
+#pragma unroll
+    for (int k = 1; k < 16; k <<= 1) s += __shfl_xor(s, k);
+    if (row < rows && c == 0) delta[row] = s;
+}
+
+size_t delta_bytes(const Window &w) { return align_up((size_t)w.batch * w.heads * w.n * sizeof(float), 256); }
+
+bool aligned16(std::initializer_list<const void *> tensors)
+{
+    for (const void *p : tensors)
+        if (((uintptr_t)p & 15u) != 0) return false;
+    return true;
+}
+
+}  // namespace
+}  // namespace psf
+
+using namespace psf;
+
+extern "C" {
+
+psf_status psf_check_window_desc(const psf_window_desc *desc)
+{
+    Window w;
+    return make_window(desc, &w);
+}
+
+psf_status psf_window_attn_fwd(const psf_window_desc *desc, const void *Q, const void *K, const void *V, const int32_t *lengths,
+                               void *O, float *lse, void *hip_stream)
+{
+    Window w;
+    const psf_status st = make_window(desc, &w);
+    if (st != PSF_OK) return st;
+    if (!Q || !K || !V || !O) return PSF_ERR_NULL;
+    if (!aligned16({Q, K, V, O})) return PSF_ERR_ALIGNMENT;
+    WindowPtrs p = {};
+    p.Q = Q; p.K = K; p.V = V; p.lengths = lengths;
+    return window_parts_fwd(w, p, O, lse, (hipStream_t)hip_stream);
+}
+
+size_t psf_window_attn_bwd_workspace_bytes(const psf_window_desc *desc)
+{
+    Window w;
+    if (make_window(desc, &w) != PSF_OK) return 0;
+    return delta_bytes(w) + align_up(window_parts_room(w), 256);
+}
+
+psf_status psf_window_attn_bwd(const psf_window_desc *desc, const void *Q, const void *K, const void *V, const int32_t *lengths,
+                               const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV, void *workspace,
+                               size_t workspace_bytes, void *hip_stream)
+{
+    Window w;
+    psf_status st = make_window(desc, &w);
+    if (st != PSF_OK) return st;
+    if (!Q || !K || !V || !O || !lse || !dO || !dQ || !dK || !dV || !workspace) return PSF_ERR_NULL;
+    if (workspace_bytes < psf_window_attn_bwd_workspace_bytes(desc)) return PSF_ERR_WORKSPACE;
+    if (((uintptr_t)workspace & 255u) != 0) return PSF_ERR_WORKSPACE;
+    if (!aligned16({Q, K, V, O, dO, dQ, dK, dV})) return PSF_ERR_ALIGNMENT;
+    hipStream_t s = (hipStream_t)hip_stream;
+    WindowPtrs p = {};
+    p.Q = Q; p.K = K; p.V = V; p.O = O; p.dO = dO; p.lengths = lengths; p.lse = lse;
+    p.dQ = dQ; p.dK = dK; p.dV = dV;
+    float *delta = (float *)workspace;
+    p.delta = delta;
+    p.room = (float *)((char *)workspace + delta_bytes(w));
+    const int64_t rows = (int64_t)w.batch * w.heads * w.n;
+    const dim3 grid((uint32_t)((rows + 15) / 16));
+    if (w.bf16) hipLaunchKernelGGL((window_delta_kernel<bf16_t>), grid, dim3(256), 0, s, (const bf16_t *)O, (const bf16_t *)dO, delta, w, rows);
+    else hipLaunchKernelGGL((window_delta_kernel<float>), grid, dim3(256), 0, s, (const float *)O, (const float *)dO, delta, w, rows);
+    PSF_LAUNCH_CHECK();
+    return window_parts_bwd(w, p, s);
+}
+
+}  // extern "C"

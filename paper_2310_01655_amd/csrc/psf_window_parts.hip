@@ -1,0 +1,318 @@
+// Window attention on bf16 parts of fp32 values (psf_parts.h): three parts of a value in fp32 storage, one of
+// a value in bf16 storage, weights in three.  A wave owns 16 rows as the columns of its results; tiles of 32 rows
+// of the other side go through LDS, where they are read along their rows for the scores and
+// transposed for the sums.  Bound by the six products that stand for one fp32 product.
+#include "psf_parts.h"
+#include "psf_window.h"
+
+namespace psf {
+namespace {
+
+constexpr int kTile = 32;
+constexpr int kRows = 64;                  // rows of a workgroup: four waves of 16
+
+// A tile of 32 rows of both operands (keys and values, or queries and output gradients) on its way into LDS.
+template <int NT, typename S>
+struct TilePair {
+    static constexpr int PITCH = row_pitch<NT>(), P = parts_of<S>(), PLANE = kTile * PITCH;
+    PartTile<NT, kTile, PITCH, S> a, b;
+    __device__ __forceinline__ void load(const S *x, const S *y, int ld, int valid, int width)
+    {
+        a.load(x, ld, valid, width);
+        b.load(y, ld, valid, width);
+    }
+    // Returns bit 0 when the first operand, bit 1 when the second has shown an infinity or NaN to the workgroup so far
+    // (`seen` in LDS, zero before the first tile).
+    __device__ __forceinline__ int store(uint16_t *to_a, uint16_t *to_b, int valid, int width, int *seen) const
+    {
+        const bool odd_a = a.template store<true>(to_a, valid, width), odd_b = b.template store<true>(to_b, valid, width);
+        if (odd_a || odd_b) atomicOr(seen, (odd_a ? 1 : 0) | (odd_b ? 2 : 0));
+        __syncthreads();
+        return *seen;
+    }
+};
+
+__device__ __forceinline__ float max_over_groups(float x)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// acc += tile^T w for this lane's eight places of the tile (tile order); seen: bit k for tile row k
+template <int NT, int P>
+__device__ __forceinline__ void add_tile(const uint16_t *tile, int plane, int pitch, const float (&w8)[8], f4 (&acc)[NT], int lane,
+                                         bool odd, unsigned seen)
+{
+    if (odd) add_parts_odd<NT, P>(tile, plane, pitch, w8, acc, lane, seen);
+    else {
+        Parts<3> w;
+        split8(w8, w);
+        add_parts<NT, P>(tile, plane, pitch, w, acc, lane);
+        settle_parts();
+    }
+}
+
+// bits of the tile's rows that row `i` (as a query) sees, keys from j0 on
+__device__ __forceinline__ unsigned seen_keys(const Window &w, int i, int j0, int end)
+{
+    unsigned m = 0;
+    if (i < end)
+        for (int k = 0; k < kTile; ++k) m |= window_sees(w, i, j0 + k) ? 1u << k : 0u;
+    return m;
+}
+// bits of the tile's rows (as queries from i0 on) that see key j
+__device__ __forceinline__ unsigned seen_by(const Window &w, int j, int i0, int end)
+{
+    unsigned m = 0;
+    for (int k = 0; k < kTile; ++k) m |= i0 + k < end && window_sees(w, i0 + k, j) ? 1u << k : 0u;
+    return m;
+}
+
+template <int NT, typename S>
+__global__ __launch_bounds__(256) void window_parts_fwd_kernel(const S *Q, const S *K, const S *V, const int32_t *lengths, S *O,
+                                                               float *lse, Window w)
+{
+    constexpr int KS = NT / 2, P = parts_of<S>();
+    using Tiles = TilePair<NT, S>;
+    __shared__ uint16_t tk[P * Tiles::PLANE], tv[P * Tiles::PLANE];
+    __shared__ int odd_seen;
+    if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int b = blockIdx.y / w.heads, h = blockIdx.y % w.heads, d = w.d;
+    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, i = first + 16 * wave + li;
+    const int64_t at_q = b * w.batch_q + h * w.head_q, at_k = b * w.batch_k + h / w.group * w.head_k;
+    f4 acc[NT];
+    clear(acc);
+    float top = -INFINITY, sum = 0.f;
+    if (first < end) {                                     // (the same in the whole workgroup)
+        Parts<P> own[KS];
+        {
+            OwnRow<KS, S> row;
+            row.load(Q + at_q + (i < end ? i : end - 1) * w.row_q, d, 1, g);
+            row.parts(own, d, g);
+        }
+        const int last = first + kRows < end ? first + kRows - 1 : end - 1;
+        const KeyTiles tiles(w, first, last, kTile);
+        Tiles next;
+        auto load = [&](int k) {
+            const int j0 = tiles.at(k) * kTile;
+            next.load(K + at_k + j0 * w.row_k, V + at_k + j0 * w.row_k, (int)w.row_k, end - j0, d);
+        };
+        load(0);
+        for (int k = 0; k < tiles.total; ++k) {
+            const int j0 = tiles.at(k) * kTile;
+            __syncthreads();
+            const int odd = next.store(tk, tv, end - j0, d, &odd_seen);
+            if (k + 1 < tiles.total) load(k + 1);
+            f4 s[2];
+            score_parts<2, KS, P, P>(tk, Tiles::PLANE, Tiles::PITCH, 0, own, lane, s);
+            float w8[8], most = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = j0 + 16 * (e / 4) + 4 * g + e % 4;
+                w8[e] = i < end && window_sees(w, i, j) ? s[e / 4][e % 4] * w.scale2 : -INFINITY;
+                most = fmaxf(most, w8[e]);
+            }
+            most = fmaxf(top, max_over_groups(most));
+            const float less = top == -INFINITY ? 0.f : exp2f(top - most), base = most == -INFINITY ? 0.f : most;
+            top = most;
+            sum *= less;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[t] *= less;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w8[e] = exp2f(w8[e] - base);
+                sum += w8[e];
+            }
+            add_tile<NT, P>(tv, Tiles::PLANE, Tiles::PITCH, w8, acc, lane, odd & 2, odd & 2 ? seen_keys(w, i, j0, end) : 0u);
+        }
+    }
+    sum = over_groups(sum);
+    if (i >= w.n) return;
+    const float by = i < end ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) store_piece(O + at_q + i * w.row_q, 16 * t + 4 * g, d, 1, acc[t] * by);
+    if (lse && g == 0) lse[((size_t)b * w.heads + h) * w.n + i] = i < end ? (top + log2f(sum)) * kWindowLn2 : -INFINITY;
+}
+
+// dQ: as forward, a wave owns 16 queries.
+template <int NT, typename S>
+__global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const S *K, const S *V, const S *dO,
+                                                              const int32_t *lengths, const float *lse, const float *delta, S *dQ,
+                                                              Window w)
+{
+    constexpr int KS = NT / 2, P = parts_of<S>();
+    using Tiles = TilePair<NT, S>;
+    __shared__ uint16_t tk[P * Tiles::PLANE], tv[P * Tiles::PLANE];
+    __shared__ int odd_seen;
+    if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int b = blockIdx.y / w.heads, h = blockIdx.y % w.heads, d = w.d;
+    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, i = first + 16 * wave + li;
+    const int64_t at_q = b * w.batch_q + h * w.head_q, at_k = b * w.batch_k + h / w.group * w.head_k;
+    f4 acc[NT];
+    clear(acc);
+    if (first < end) {
+        const int safe = i < end ? i : end - 1;
+        Parts<P> own[KS], own_g[KS];
+        {
+            OwnRow<KS, S> row, row_g;
+            row.load(Q + at_q + safe * w.row_q, d, 1, g);
+            row_g.load(dO + at_q + safe * w.row_q, d, 1, g);
+            row.parts(own, d, g);
+            row_g.parts(own_g, d, g);
+        }
+        const size_t row = ((size_t)b * w.heads + h) * w.n + safe;
+        const float L = lse[row] * kWindowLog2e, D = delta[row];
+        const int last = first + kRows < end ? first + kRows - 1 : end - 1;
+        const KeyTiles tiles(w, first, last, kTile);
+        Tiles next;
+        auto load = [&](int k) {
+            const int j0 = tiles.at(k) * kTile;
+            next.load(K + at_k + j0 * w.row_k, V + at_k + j0 * w.row_k, (int)w.row_k, end - j0, d);
+        };
+        load(0);
+        for (int k = 0; k < tiles.total; ++k) {
+            const int j0 = tiles.at(k) * kTile;
+            __syncthreads();
+            const int odd = next.store(tk, tv, end - j0, d, &odd_seen);
+            if (k + 1 < tiles.total) load(k + 1);
+            f4 s[2], t[2];
+            score_parts<2, KS, P, P>(tk, Tiles::PLANE, Tiles::PITCH, 0, own, lane, s);
+            score_parts<2, KS, P, P>(tv, Tiles::PLANE, Tiles::PITCH, 0, own_g, lane, t);
+            float w8[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = j0 + 16 * (e / 4) + 4 * g + e % 4;
+                const float p = exp2f(s[e / 4][e % 4] * w.scale2 - L);
+                w8[e] = i < end && window_sees(w, i, j) ? p * (t[e / 4][e % 4] - D) : 0.f;
+            }
+            add_tile<NT, P>(tk, Tiles::PLANE, Tiles::PITCH, w8, acc, lane, odd & 1, odd & 1 ? seen_keys(w, i, j0, end) : 0u);
+        }
+    }
+    if (i >= w.n) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) store_piece(dQ + at_q + i * w.row_q, 16 * t + 4 * g, d, 1, acc[t] * w.scale);
+}
+
+// dK, dV: a wave owns 16 keys, tiles of 32 queries pass, head after head of the group.
+template <int NT, typename S>
+__global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const S *K, const S *V, const S *dO,
+                                                               const int32_t *lengths, const float *lse, const float *delta,
+                                                               S *dK, S *dV, Window w)
+{
+    constexpr int KS = NT / 2, P = parts_of<S>();
+    using Tiles = TilePair<NT, S>;
+    __shared__ uint16_t tq[P * Tiles::PLANE], tg[P * Tiles::PLANE];
+    __shared__ float rows_l[kTile], rows_d[kTile];
+    __shared__ int odd_seen;
+    if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int b = blockIdx.y / w.kv_heads, kv = blockIdx.y % w.kv_heads, d = w.d;
+    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, j = first + 16 * wave + li;
+    const int64_t at_k = b * w.batch_k + kv * w.head_k;
+    f4 acc_k[NT], acc_v[NT];
+    clear(acc_k);
+    clear(acc_v);
+    if (first < end) {
+        const int safe = j < end ? j : end - 1;
+        Parts<P> own[KS], own_v[KS];
+        {
+            OwnRow<KS, S> row, row_v;
+            row.load(K + at_k + safe * w.row_k, d, 1, g);
+            row_v.load(V + at_k + safe * w.row_k, d, 1, g);
+            row.parts(own, d, g);
+            row_v.parts(own_v, d, g);
+        }
+        // queries that see one of the keys: [first, last]
+        const int64_t reach = first < w.sinks ? end - 1 : (int64_t)first + kRows - 1 + w.window - 1;
+        const int last = reach < end ? (int)reach : end - 1;
+        const int tile0 = first / kTile, per = last / kTile + 1 - tile0, total = per * w.group;
+        Tiles next;
+        float next_l = 0.f, next_d = 0.f;
+        auto load = [&](int k) {
+            const int h = kv * w.group + k / per, i0 = (tile0 + k % per) * kTile;
+            const int64_t at = b * w.batch_q + h * w.head_q + i0 * w.row_q;
+            next.load(Q + at, dO + at, (int)w.row_q, end - i0, d);
+            if (threadIdx.x < kTile && i0 + (int)threadIdx.x < end) {
+                const size_t row = ((size_t)b * w.heads + h) * w.n + i0 + threadIdx.x;
+                next_l = lse[row];
+                next_d = delta[row];
+            }
+        };
+        load(0);
+        for (int k = 0; k < total; ++k) {
+            const int i0 = (tile0 + k % per) * kTile;
+            __syncthreads();
+            if (threadIdx.x < kTile) {
+                rows_l[threadIdx.x] = next_l * kWindowLog2e;
+                rows_d[threadIdx.x] = next_d;
+            }
+            const int odd = next.store(tq, tg, end - i0, d, &odd_seen);
+            if (k + 1 < total) load(k + 1);
+            f4 s[2], t[2];
+            score_parts<2, KS, P, P>(tq, Tiles::PLANE, Tiles::PITCH, 0, own, lane, s);
+            score_parts<2, KS, P, P>(tg, Tiles::PLANE, Tiles::PITCH, 0, own_v, lane, t);
+            float p8[8], w8[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = 16 * (e / 4) + 4 * g + e % 4, i = i0 + r;
+                const bool seen = i < end && j < end && window_sees(w, i, j);
+                p8[e] = seen ? exp2f(s[e / 4][e % 4] * w.scale2 - rows_l[r]) : 0.f;
+                w8[e] = seen ? p8[e] * (t[e / 4][e % 4] - rows_d[r]) : 0.f;
+            }
+            const unsigned seen = odd && j < end ? seen_by(w, j, i0, end) : 0u;
+            add_tile<NT, P>(tg, Tiles::PLANE, Tiles::PITCH, p8, acc_v, lane, odd & 2, seen);
+            add_tile<NT, P>(tq, Tiles::PLANE, Tiles::PITCH, w8, acc_k, lane, odd & 1, seen);
+        }
+    }
+    if (j >= w.n) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        store_piece(dK + at_k + j * w.row_k, 16 * t + 4 * g, d, 1, acc_k[t] * w.scale);
+        store_piece(dV + at_k + j * w.row_k, 16 * t + 4 * g, d, 1, acc_v[t]);
+    }
+}
+
+template <class F>
+psf_status with_type(const Window &w, F &&go)
+{
+    if (w.bf16) return w.d <= 64 ? go(std::integral_constant<int, 4>{}, bf16_t{}) : go(std::integral_constant<int, 8>{}, bf16_t{});
+    return w.d <= 64 ? go(std::integral_constant<int, 4>{}, float{}) : go(std::integral_constant<int, 8>{}, float{});
+}
+
+}  // namespace
+
+psf_status window_parts_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s)
+{
+    return with_type(w, [&](auto nt, auto type) -> psf_status {
+        constexpr int NT = decltype(nt)::value;
+        typedef decltype(type) S;
+        hipLaunchKernelGGL((window_parts_fwd_kernel<NT, S>), dim3((w.n + kRows - 1) / kRows, w.batch * w.heads), dim3(256), 0, s,
+                           (const S *)p.Q, (const S *)p.K, (const S *)p.V, p.lengths, (S *)O, lse, w);
+        PSF_LAUNCH_CHECK();
+        return PSF_OK;
+    });
+}
+
+size_t window_parts_room(const Window &) { return 0; }
+
+psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
+{
+    return with_type(w, [&](auto nt, auto type) -> psf_status {
+        constexpr int NT = decltype(nt)::value;
+        typedef decltype(type) S;
+        const unsigned tiles = (w.n + kRows - 1) / kRows;
+        hipLaunchKernelGGL((window_parts_dkv_kernel<NT, S>), dim3(tiles, w.batch * w.kv_heads), dim3(256), 0, s, (const S *)p.Q,
+                           (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dK, (S *)p.dV, w);
+        PSF_LAUNCH_CHECK();
+        hipLaunchKernelGGL((window_parts_dq_kernel<NT, S>), dim3(tiles, w.batch * w.heads), dim3(256), 0, s, (const S *)p.Q,
+                           (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dQ, w);
+        PSF_LAUNCH_CHECK();
+        return PSF_OK;
+    });
+}
+
+}  // namespace psf
