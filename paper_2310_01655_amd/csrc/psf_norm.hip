@@ -133,77 +133,80 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_kernel(const T *x, cons
     constexpr int N = Piece<T>::N, ROWS = kNormThreads / G;
     __shared__ float lds[4][R];
     const int lane = threadIdx.x % G;
-    const int64_t first = (int64_t)blockIdx.x * (ROWS * R) + threadIdx.x / G;
     const float inv_w = 1.0f / (float)width;
-    typename Piece<T>::raw raw[R][PER];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t row = first + r * ROWS;
-        const T *src = x + (row < rows ? row : rows - 1) * width;      // (rows that are not there: the last one, unused)
-#pragma unroll
-        for (int k = 0; k < PER; ++k)
-            if ((k * G + lane) * N < width) raw[r][k] = norm_load(src, (k * G + lane) * N, width);
-    }
-    float s[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        s[r] = 0.f;
-#pragma unroll
-        for (int k = 0; k < PER; ++k)
-            if ((k * G + lane) * N < width) {
-                float v[N];
-                Piece<T>::get(raw[r][k], v);
-#pragma unroll
-                for (int e = 0; e < N; ++e) s[r] += v[e];              // (zeros behind the row)
-            }
-    }
-    sum_row<G, R>(s, lds);
-    float mean[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        mean[r] = s[r] * inv_w;
-        s[r] = 0.f;
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int c = (k * G + lane) * N;
-            if (c < width) {
-                float v[N];
-                Piece<T>::get(raw[r][k], v);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float t = c + e < width ? v[e] - mean[r] : 0.f;
-                    s[r] += t * t;
-                }
-            }
-        }
-    }
-    sum_row<G, R>(s, lds);
-    float inv[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        inv[r] = 1.0f / sqrtf(s[r] * inv_w + eps);
-        const int64_t row = first + r * ROWS;
-        if (stats && lane == 0 && row < rows) stats[row] = make_float2(mean[r], inv[r]);
-    }
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int c = (k * G + lane) * N;
-        if (c >= width) continue;
-        float w[N], b[N];
-        Piece<T>::get(norm_load(weight, c, width), w);
-        if (bias) Piece<T>::get(norm_load(bias, c, width), b);
-        else
-#pragma unroll
-            for (int e = 0; e < N; ++e) b[e] = 0.f;
+    // (one pass but for calls of more rows than a launch has workgroups for)
+    for (int64_t at = (int64_t)blockIdx.x * (ROWS * R); at < rows; at += (int64_t)gridDim.x * (ROWS * R)) {
+        const int64_t first = at + threadIdx.x / G;
+        typename Piece<T>::raw raw[R][PER];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = first + r * ROWS;
-            if (row >= rows) continue;
-            float v[N];
-            Piece<T>::get(raw[r][k], v);
+            const T *src = x + (row < rows ? row : rows - 1) * width;      // (rows that are not there: the last one, unused)
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = (v[e] - mean[r]) * inv[r] * w[e] + b[e];
-            norm_store(y + row * width, c, width, v);
+            for (int k = 0; k < PER; ++k)
+                if ((k * G + lane) * N < width) raw[r][k] = norm_load(src, (k * G + lane) * N, width);
+        }
+        float s[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            s[r] = 0.f;
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if ((k * G + lane) * N < width) {
+                    float v[N];
+                    Piece<T>::get(raw[r][k], v);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s[r] += v[e];              // (zeros behind the row)
+                }
+        }
+        sum_row<G, R>(s, lds);
+        float mean[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = s[r] * inv_w;
+            s[r] = 0.f;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int c = (k * G + lane) * N;
+                if (c < width) {
+                    float v[N];
+                    Piece<T>::get(raw[r][k], v);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float t = c + e < width ? v[e] - mean[r] : 0.f;
+                        s[r] += t * t;
+                    }
+                }
+            }
+        }
+        sum_row<G, R>(s, lds);
+        float inv[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            inv[r] = 1.0f / sqrtf(s[r] * inv_w + eps);
+            const int64_t row = first + r * ROWS;
+            if (stats && lane == 0 && row < rows) stats[row] = make_float2(mean[r], inv[r]);
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int c = (k * G + lane) * N;
+            if (c >= width) continue;
+            float w[N], b[N];
+            Piece<T>::get(norm_load(weight, c, width), w);
+            if (bias) Piece<T>::get(norm_load(bias, c, width), b);
+            else
+#pragma unroll
+                for (int e = 0; e < N; ++e) b[e] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int64_t row = first + r * ROWS;
+                if (row >= rows) continue;
+                float v[N];
+                Piece<T>::get(raw[r][k], v);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = (v[e] - mean[r]) * inv[r] * w[e] + b[e];
+                norm_store(y + row * width, c, width, v);
+            }
         }
     }
 }
@@ -367,8 +370,8 @@ psf_status fwd_launch(int64_t rows, int width, float eps, const void *x, const v
 {
     return norm_shape<T>(width, [&](auto g, auto per) -> psf_status {
         constexpr int G = decltype(g)::value, PER = decltype(per)::value, R = rows_fwd<PER>();
-        const int64_t each = kNormThreads / G * R;
-        hipLaunchKernelGGL((norm_fwd_kernel<T, G, PER, R>), dim3((uint32_t)((rows + each - 1) / each)), dim3(kNormThreads), 0, s,
+        const int64_t each = kNormThreads / G * R, need = (rows + each - 1) / each, most = 1 << 23;   // (work-items below 2^32)
+        hipLaunchKernelGGL((norm_fwd_kernel<T, G, PER, R>), dim3((uint32_t)(need < most ? need : most)), dim3(kNormThreads), 0, s,
                            (const T *)x, (const T *)weight, (const T *)bias, (T *)y, (float2 *)stats, rows, width, eps);
         PSF_LAUNCH_CHECK();
         return PSF_OK;

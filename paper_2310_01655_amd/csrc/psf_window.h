@@ -24,7 +24,8 @@ struct Window {
 struct WindowPtrs {
     const void *Q, *K, *V, *O, *dO;
     const int32_t *lengths;
-    const float *lse, *delta;
+    const float *lse;
+    float *delta;                          // [batch, heads, n]
     void *dQ, *dK, *dV;
     float *room;                           // shares of gradients that several workgroups form
 };
@@ -57,9 +58,12 @@ struct KeyTiles {
     __device__ __forceinline__ int at(int k) const { return k < few ? k : window_first + k - few; }
 };
 
+psf_status window_bf16_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s);
+psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s);
+size_t window_bf16_room(const Window &w);              // bytes of WindowPtrs::room
 psf_status window_parts_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s);
 psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s);
-size_t window_parts_room(const Window &w);             // bytes of WindowPtrs::room
+size_t window_parts_room(const Window &w);
 
 }  // namespace psf
 #endif

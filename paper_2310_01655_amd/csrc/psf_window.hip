@@ -1,4 +1,4 @@
-// Entry points of the window attention: the descriptor's check, the choice of kernels, D = <dO, O>.
+// Entry points of the window attention: the descriptor's check, the choice of kernels.
 #include <initializer_list>
 #include "psf_window.h"
 
@@ -18,12 +18,15 @@ psf_status make_window(const psf_window_desc *desc, Window *out)
     // lie within 4 GB of each other
     if ((long long)desc->batch * desc->heads > 65535 || desc->n > (1 << 24) || (long long)desc->heads * desc->d > (1 << 20))
         return PSF_ERR_UNSUPPORTED;
+    // a launch holds fewer than 2^32 work-items: 256 for 64 rows
+    if ((long long)desc->batch * desc->heads * ((desc->n + 63) / 64) > (1 << 23)) return PSF_ERR_UNSUPPORTED;
     Window w;
     w.batch = desc->batch; w.heads = desc->heads; w.kv_heads = desc->kv_heads; w.group = desc->heads / desc->kv_heads;
     w.n = desc->n; w.d = desc->d;
     w.window = desc->window < desc->n ? desc->window : desc->n;
     w.sinks = desc->sinks < desc->n ? desc->sinks : desc->n;
     w.bf16 = desc->dtype == PSF_BF16;
+    if (!(fabsf(desc->scale) < INFINITY)) return PSF_ERR_UNSUPPORTED;
     w.scale = desc->scale;
     w.scale2 = desc->scale * kWindowLog2e;
     const int64_t n = w.n, d = w.d;
@@ -32,24 +35,6 @@ psf_status make_window(const psf_window_desc *desc, Window *out)
     w.batch_k = n * w.kv_heads * d; w.head_k = tokens ? d : n * d; w.row_k = tokens ? w.kv_heads * d : d;
     *out = w;
     return PSF_OK;
-}
-
-// D of every row: 16 lanes a row, 8 columns a lane.
-template <typename S>
-__global__ __launch_bounds__(256) void window_delta_kernel(const S *O, const S *dO, float *delta, Window w, int64_t rows)
-{
-    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const int c = 8 * (threadIdx.x % 16);
-    float s = 0.f;
-    if (row < rows && c < w.d) {
-        const int64_t unit = row / w.n, i = row - unit * w.n, b = unit / w.heads, h = unit - b * w.heads;
-        const int64_t at = b * w.batch_q + h * w.head_q + i * w.row_q + c;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += load_f(O, at + k) * load_f(dO, at + k);
-    }
-#pragma unroll
-    for (int k = 1; k < 16; k <<= 1) s += __shfl_xor(s, k);
-    if (row < rows && c == 0) delta[row] = s;
 }
 
 size_t delta_bytes(const Window &w) { return align_up((size_t)w.batch * w.heads * w.n * sizeof(float), 256); }
@@ -84,14 +69,14 @@ psf_status psf_window_attn_fwd(const psf_window_desc *desc, const void *Q, const
     if (!aligned16({Q, K, V, O})) return PSF_ERR_ALIGNMENT;
     WindowPtrs p = {};
     p.Q = Q; p.K = K; p.V = V; p.lengths = lengths;
-    return window_parts_fwd(w, p, O, lse, (hipStream_t)hip_stream);
+    return w.bf16 ? window_bf16_fwd(w, p, O, lse, (hipStream_t)hip_stream) : window_parts_fwd(w, p, O, lse, (hipStream_t)hip_stream);
 }
 
 size_t psf_window_attn_bwd_workspace_bytes(const psf_window_desc *desc)
 {
     Window w;
     if (make_window(desc, &w) != PSF_OK) return 0;
-    return delta_bytes(w) + align_up(window_parts_room(w), 256);
+    return delta_bytes(w) + align_up(w.bf16 ? window_bf16_room(w) : window_parts_room(w), 256);
 }
 
 psf_status psf_window_attn_bwd(const psf_window_desc *desc, const void *Q, const void *K, const void *V, const int32_t *lengths,
@@ -109,15 +94,9 @@ psf_status psf_window_attn_bwd(const psf_window_desc *desc, const void *Q, const
     WindowPtrs p = {};
     p.Q = Q; p.K = K; p.V = V; p.O = O; p.dO = dO; p.lengths = lengths; p.lse = lse;
     p.dQ = dQ; p.dK = dK; p.dV = dV;
-    float *delta = (float *)workspace;
-    p.delta = delta;
+    p.delta = (float *)workspace;
     p.room = (float *)((char *)workspace + delta_bytes(w));
-    const int64_t rows = (int64_t)w.batch * w.heads * w.n;
-    const dim3 grid((uint32_t)((rows + 15) / 16));
-    if (w.bf16) hipLaunchKernelGGL((window_delta_kernel<bf16_t>), grid, dim3(256), 0, s, (const bf16_t *)O, (const bf16_t *)dO, delta, w, rows);
-    else hipLaunchKernelGGL((window_delta_kernel<float>), grid, dim3(256), 0, s, (const float *)O, (const float *)dO, delta, w, rows);
-    PSF_LAUNCH_CHECK();
-    return window_parts_bwd(w, p, s);
+    return w.bf16 ? window_bf16_bwd(w, p, s) : window_parts_bwd(w, p, s);
 }
 
 }  // extern "C"

@@ -1,5 +1,4 @@
-// Window attention on bf16 parts of fp32 values (psf_parts.h): three parts of a value in fp32 storage, one of
-// a value in bf16 storage, weights in three.  A wave owns 16 rows as the columns of its results; tiles of 32 rows
+// Window attention in fp32 storage on bf16 parts of its values (psf_parts.h): three parts of every value and weight.  A wave owns 16 rows as the columns of its results; tiles of 32 rows
 // of the other side go through LDS, where they are read along their rows for the scores and
 // transposed for the sums.  Bound by the six products that stand for one fp32 product.
 #include "psf_parts.h"
@@ -137,10 +136,10 @@ __global__ __launch_bounds__(256) void window_parts_fwd_kernel(const S *Q, const
     if (lse && g == 0) lse[((size_t)b * w.heads + h) * w.n + i] = i < end ? (top + log2f(sum)) * kWindowLn2 : -INFINITY;
 }
 
-// dQ: as forward, a wave owns 16 queries.
+// dQ: as forward, a wave owns 16 queries; and D = <dO, o> of every row for the kernel below.
 template <int NT, typename S>
-__global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const S *K, const S *V, const S *dO,
-                                                              const int32_t *lengths, const float *lse, const float *delta, S *dQ,
+__global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const S *K, const S *V, const S *O, const S *dO,
+                                                              const int32_t *lengths, const float *lse, float *delta, S *dQ,
                                                               Window w)
 {
     constexpr int KS = NT / 2, P = parts_of<S>();
@@ -157,15 +156,25 @@ __global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const 
     if (first < end) {
         const int safe = i < end ? i : end - 1;
         Parts<P> own[KS], own_g[KS];
+        float D = 0.f;
         {
-            OwnRow<KS, S> row, row_g;
+            OwnRow<KS, S> row, row_g, row_o;
             row.load(Q + at_q + safe * w.row_q, d, 1, g);
             row_g.load(dO + at_q + safe * w.row_q, d, 1, g);
+            row_o.load(O + at_q + safe * w.row_q, d, 1, g);
             row.parts(own, d, g);
             row_g.parts(own_g, d, g);
+#pragma unroll
+            for (int e = 0; e < 2 * KS; ++e) {
+                const f4 x = row_g.at(e, d, g), y = row_o.at(e, d, g);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) D += x[k] * y[k];
+            }
         }
+        D = over_groups(D);
         const size_t row = ((size_t)b * w.heads + h) * w.n + safe;
-        const float L = lse[row] * kWindowLog2e, D = delta[row];
+        const float L = lse[row] * kWindowLog2e;
+        if (i < end && g == 0) delta[row] = D;
         const int last = first + kRows < end ? first + kRows - 1 : end - 1;
         const KeyTiles tiles(w, first, last, kTile);
         Tiles next;
@@ -277,19 +286,18 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
 }
 
 template <class F>
-psf_status with_type(const Window &w, F &&go)
+psf_status with_width(const Window &w, F &&go)
 {
-    if (w.bf16) return w.d <= 64 ? go(std::integral_constant<int, 4>{}, bf16_t{}) : go(std::integral_constant<int, 8>{}, bf16_t{});
-    return w.d <= 64 ? go(std::integral_constant<int, 4>{}, float{}) : go(std::integral_constant<int, 8>{}, float{});
+    return w.d <= 64 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 8>{});
 }
 
 }  // namespace
 
 psf_status window_parts_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s)
 {
-    return with_type(w, [&](auto nt, auto type) -> psf_status {
+    return with_width(w, [&](auto nt) -> psf_status {
         constexpr int NT = decltype(nt)::value;
-        typedef decltype(type) S;
+        typedef float S;
         hipLaunchKernelGGL((window_parts_fwd_kernel<NT, S>), dim3((w.n + kRows - 1) / kRows, w.batch * w.heads), dim3(256), 0, s,
                            (const S *)p.Q, (const S *)p.K, (const S *)p.V, p.lengths, (S *)O, lse, w);
         PSF_LAUNCH_CHECK();
@@ -301,15 +309,15 @@ size_t window_parts_room(const Window &) { return 0; }
 
 psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
 {
-    return with_type(w, [&](auto nt, auto type) -> psf_status {
+    return with_width(w, [&](auto nt) -> psf_status {
         constexpr int NT = decltype(nt)::value;
-        typedef decltype(type) S;
+        typedef float S;
         const unsigned tiles = (w.n + kRows - 1) / kRows;
+        hipLaunchKernelGGL((window_parts_dq_kernel<NT, S>), dim3(tiles, w.batch * w.heads), dim3(256), 0, s, (const S *)p.Q,
+                           (const S *)p.K, (const S *)p.V, (const S *)p.O, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dQ, w);
+        PSF_LAUNCH_CHECK();
         hipLaunchKernelGGL((window_parts_dkv_kernel<NT, S>), dim3(tiles, w.batch * w.kv_heads), dim3(256), 0, s, (const S *)p.Q,
                            (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dK, (S *)p.dV, w);
-        PSF_LAUNCH_CHECK();
-        hipLaunchKernelGGL((window_parts_dq_kernel<NT, S>), dim3(tiles, w.batch * w.heads), dim3(256), 0, s, (const S *)p.Q,
-                           (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dQ, w);
         PSF_LAUNCH_CHECK();
         return PSF_OK;
     });
