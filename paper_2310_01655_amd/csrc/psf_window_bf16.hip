@@ -130,12 +130,35 @@ __device__ __forceinline__ bool none_seen(const Window &w, int i0, int j0, int l
     return j0 > i0 + kOwn - 1 || (i0 - (j0 + len - 1) >= w.window && j0 >= w.sinks);
 }
 
-// Workgroups of a unit follow each other on one XCD (they are dealt out to the 8 XCDs in turn), so that its L2 serves the
-// tiles that neighbouring rows share.
+// Which workgroup of the call (unit by unit, neighbouring rows side by side) workgroup `id` of the launch is.  The launch
+// deals its workgroups out to the 8 XCDs in turn; runs of 16 neighbours stay on one XCD, whose L2 serves the
+// tiles that they share, and the runs go round the XCDs, so that sequences of unequal length load all of them.
 __device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t total)
 {
-    const uint32_t each = total / 8;
-    return id < 8 * each ? id % 8 * each + id / 8 : id;
+    constexpr uint32_t RUN = 16;
+    if (id >= total / (8 * RUN) * (8 * RUN)) return id;
+    const uint32_t slot = id / 8;
+    return (slot / RUN * 8 + id % 8) * RUN + slot % RUN;
+}
+
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+// keys j0 .. j0 + 31 that row i sees, as bits
+__device__ __forceinline__ uint32_t seen_keys(const Window &w, int i, int j0)
+{
+    return bits_below(i - j0 + 1) & (~bits_below(i - w.window + 1 - j0) | bits_below(w.sinks - j0));
+}
+// rows i0 .. i0 + 31 below `end` that see key j, as bits
+__device__ __forceinline__ uint32_t seen_by(const Window &w, int j, int i0, int end)
+{
+    const int64_t reach = j < w.sinks ? (int64_t)end : (int64_t)j + w.window;
+    return bits_below((reach < end ? (int)reach : end) - i0) & ~bits_below(j - i0);
+}
+// x where bit place(e, h) of `bits` >> 4 h is set, `other` elsewhere
+template <int E>
+__device__ __forceinline__ float pick(uint32_t bits_h, float x, uint32_t other)
+{
+    const uint32_t mask = (uint32_t)__builtin_amdgcn_sbfe((int)bits_h, 8 * (E / 4) + E % 4, 1);
+    return __uint_as_float((__float_as_uint(x) & mask) | (other & ~mask));
 }
 
 // Row i again, pair by pair in fp32 and without a masked pair: for rows whose result is not finite, so that an infinity
@@ -223,10 +246,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
             for (int t = 0; t < 2; ++t) s[t] = scores<D>(at, tk, t, own);
             if (!all_seen(w, i0, j0, kTile)) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (!window_sees(w, i, j0 + 32 * t + place(e, h))) s[t][e] = -INFINITY;
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t bits = seen_keys(w, i, j0 + 32 * t) >> (4 * h);
+                    static_for<16>([&](auto e) { s[t][int(e)] = pick<e>(bits, s[t][int(e)], 0xff800000u); });   // -inf
+                }
             }
             float most = s[0][0];
 #pragma unroll
@@ -435,9 +458,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -L)) * (u[e] - dot);
                 if (!all) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (!window_sees(w, i, j0 + 32 * t + place(e, h))) s[e] = 0.f;
+                    const uint32_t bits = seen_keys(w, i, j0 + 32 * t) >> (4 * h);
+                    static_for<16>([&](auto e) { s[int(e)] = pick<e>(bits, s[int(e)], 0u); });
                 }
                 add_turned<D>(at, tk, t, s, acc);
             }
@@ -563,11 +585,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void window_dkv_kernel(
                     u[e] = s[e] * (u[e] - r.y);
                 }
                 if (!all) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int i = i0 + 32 * t + place(e, h);
-                        if (i >= end || !window_sees(w, i, j)) s[e] = u[e] = 0.f;
-                    }
+                    const uint32_t bits = seen_by(w, j, i0 + 32 * t, end) >> (4 * h);
+                    static_for<16>([&](auto e) {
+                        s[int(e)] = pick<e>(bits, s[int(e)], 0u);
+                        u[int(e)] = pick<e>(bits, u[int(e)], 0u);
+                    });
                 }
                 add_turned<D>(at, tg, t, s, acc_v);
                 add_turned<D>(at, tq, t, u, acc_k);
