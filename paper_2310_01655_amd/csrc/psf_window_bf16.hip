@@ -18,9 +18,9 @@ constexpr int kTile = 64;                  // rows of a tile
 constexpr float kLazy = 8.0f;              // a maximum is left as it is until one above it by 2^8 comes
 
 // A tile of rows of two tensors (keys and values, or queries and output gradients), copied by the workgroup.
-template <int D>
+template <int D, int TILE = kTile>
 struct Staged {
-    static constexpr int BYTES = kTile * D * 2, COPIES = BYTES / (kThreads * 16), ROWS = kThreads * 8 / D;   // rows a copy
+    static constexpr int BYTES = TILE * D * 2, COPIES = BYTES / (kThreads * 16), ROWS = kThreads * 8 / D;   // rows a copy
     uint32_t wave_at, lane_row, lane_piece, step;          // LDS address of the wave's pieces; row, byte offset of the piece
     __device__ __forceinline__ Staged(const void *lds, int d)
     {
@@ -505,24 +505,25 @@ struct KeyWalks {
 // queries that see one of the keys from `first` on (a workgroup's): tiles [tile0, tile0 + count)
 struct QueryTiles {
     int tile0, count;
-    __host__ __device__ QueryTiles(const Window &w, int first, int end)
+    __host__ __device__ QueryTiles(const Window &w, int first, int end, int size)
     {
         const int64_t reach = first < w.sinks ? (int64_t)end - 1 : (int64_t)first + kOwnWg - 1 + w.window - 1;
         const int last = reach < end ? (int)reach : end - 1;
-        tile0 = first / kTile;
-        count = last / kTile + 1 - tile0;
+        tile0 = first / size;
+        count = last / size + 1 - tile0;
     }
 };
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void window_dkv_kernel(
+__global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
     const bf16_t *Q, const bf16_t *K, const bf16_t *V, const int32_t *lengths, const float *lse, const bf16_t *dO,
     const float *delta, bf16_t *dK, bf16_t *dV, float *room, Window w, KeyWalks walks)
 {
-    constexpr int KS = D / 16, CT = D / 32;
-    using Tile = Staged<D>;
-    __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES];
-    __shared__ float2 row_data[2][kTile];                  // L (in exponents of 2) and D of the tile's rows
+    constexpr int KS = D / 16, CT = D / 32, TILE = D == 64 ? 64 : 32;
+    constexpr bool V_IN_LDS = D == 128;
+    using Tile = Staged<D, TILE>;
+    __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES + (V_IN_LDS ? kOwnWg * D * 2 : 0)];
+    __shared__ float2 row_data[2][TILE];                  // L (in exponents of 2) and D of the tile's rows
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 31, h = lane >> 5, d = w.d;
     const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), each = walks.each(), unit = at_grid / each;
     const int which = at_grid - unit * each, shared = walks.few * walks.parts;
@@ -538,16 +539,16 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void window_dkv_kernel(
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc_k[ct] = acc_v[ct] = f32x16{0};
     if (first < end) {
-        const QueryTiles tiles(w, first, end);
+        const QueryTiles tiles(w, first, end, TILE);
         const int total = tiles.count * w.group, begin = (int)((int64_t)total * part / parts),
                   stop = (int)((int64_t)total * (part + 1) / parts);
         const Tile stage(lds, d);
         float2 next = make_float2(0.f, 0.f);
         int head = begin / tiles.count, tile = begin - head * tiles.count;     // of the next copy
         auto copy = [&](int buf) {
-            const int i0 = (tiles.tile0 + tile) * kTile;
+            const int i0 = (tiles.tile0 + tile) * TILE;
             stage.copy(Q + at_q + head * w.head_q, dO + at_q + head * w.head_q, w.row_q, i0, end, buf);
-            if (threadIdx.x < kTile) {
+            if (threadIdx.x < TILE) {
                 const size_t row = at_rows + (size_t)head * w.n + (i0 + (int)threadIdx.x < end ? i0 + (int)threadIdx.x : end - 1);
                 next = make_float2(lse[row] * kWindowLog2e, delta[row]);
             }
@@ -558,26 +559,37 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void window_dkv_kernel(
         };
         int now = tile;
         if (begin < stop) copy(0);
-        bf16x8 own[KS], own_v[KS];
-        own_row<D>(K + at_k + (j < end ? j : end - 1) * w.row_k, d, h, w.scale2, own);
-        own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, own_v);
         const Reads<D> at(lane);
+        bf16x8 own[KS], own_v[V_IN_LDS ? 1 : KS];
+        own_row<D>(K + at_k + (j < end ? j : end - 1) * w.row_k, d, h, w.scale2, own);
+        unsigned char *wave_v = lds + 2 * 2 * Tile::BYTES + wave * (kOwn * D * 2);
+        if constexpr (V_IN_LDS) {
+            bf16x8 v[KS];
+            own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, v);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) *(bf16x8 *)(wave_v + at.along[s]) = v[s];   // (read by this wave alone)
+        } else own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, own_v);
         for (int k = begin; k < stop; ++k) {
-            const int buf = (k - begin) & 1, i0 = (tiles.tile0 + now) * kTile;
+            const int buf = (k - begin) & 1, i0 = (tiles.tile0 + now) * TILE;
             now = tile;
             wait_all_memory();
-            if (threadIdx.x < kTile) row_data[buf][threadIdx.x] = next;
+            if (threadIdx.x < TILE) row_data[buf][threadIdx.x] = next;
             __syncthreads();
             if (k + 1 < stop) copy(buf ^ 1);
             // (rows behind the sequence are the last one again: masked)
-            const bool none = i0 + kTile - 1 < j0 || (i0 - (j0 + kOwn - 1) >= w.window && j0 >= w.sinks);
+            const bool none = i0 + TILE - 1 < j0 || (i0 - (j0 + kOwn - 1) >= w.window && j0 >= w.sinks);
             if (none) continue;
-            const bool all = i0 >= j0 + kOwn - 1 && (i0 + kTile - 1 - j0 < w.window || j0 + kOwn <= w.sinks) && i0 + kTile <= end;
+            const bool all = i0 >= j0 + kOwn - 1 && (i0 + TILE - 1 - j0 < w.window || j0 + kOwn <= w.sinks) && i0 + TILE <= end;
             const unsigned char *tq = lds + buf * 2 * Tile::BYTES, *tg = tq + Tile::BYTES;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < TILE / 32; ++t) {
                 f32x16 s = scores<D>(at, tq, t, own);
-                f32x16 u = scores<D>(at, tg, t, own_v);
+                f32x16 u = {0};
+#pragma unroll
+                for (int q = 0; q < KS; ++q) {
+                    if constexpr (V_IN_LDS) u = mfma32(at.row(tg, t, q), at.row(wave_v, 0, q), u);
+                    else u = mfma32(at.row(tg, t, q), own_v[q], u);
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float2 r = row_data[buf][32 * t + place(e, h)];
