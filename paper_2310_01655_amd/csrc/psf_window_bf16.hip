@@ -161,6 +161,31 @@ __device__ __forceinline__ float pick(uint32_t bits_h, float x, uint32_t other)
     return __uint_as_float((__float_as_uint(x) & mask) | (other & ~mask));
 }
 
+// This lane's part of a result row (columns 32 ct + place(e, h)) times `by`, to `row` in storage type; zeros where the row lies
+// behind its sequence.  Returns whether it holds an infinity or NaN.  (Columns from d on hold what the tile's
+// columns there held, which are the row's first ones again: no others that are odd.)
+template <int D>
+__device__ __forceinline__ bool store_row(const f32x16 (&acc)[D / 32], float by, bool there, bf16_t *row, int d, int h)
+{
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    float probe = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            f32x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[k] = there ? acc[ct][e + k] * by : 0.f;
+                probe = __builtin_fmaf(v[k], 0.f, probe);
+            }
+            const int col = 32 * ct + 2 * e + 4 * h;
+            if (col < d) *(bf16x4 *)(row + col) = __builtin_convertvector(v, bf16x4);
+        }
+    return probe != 0.f;
+}
+
 // Row i again, pair by pair in fp32 and without a masked pair: for rows whose result is not finite, so that an infinity
 // or NaN of a token that the row does not see leaves nothing in it (0 * inf in a tile's product).
 template <int D>
@@ -279,31 +304,14 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
     }
     sum = other_half(sum, false);
     const bool there = i < end;
-    const float by = there ? 1.f / sum : 0.f;
-    bool odd = false;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            acc[ct][e] *= by;
-            if (32 * ct + place(e, h) < d) odd |= !(fabsf(acc[ct][e]) < INFINITY);
-        }
     bf16_t *o = O + b * w.batch_q + head * w.head_q;
+    bool odd = false;
     if (i < w.n) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int col = 32 * ct + place(e, h);
-                if (col < d)
-                    *(uint2 *)(o + i * w.row_q + col) = make_uint2(
-                        (uint32_t)f32_to_bf16(acc[ct][e]) | (uint32_t)f32_to_bf16(acc[ct][e + 1]) << 16,
-                        (uint32_t)f32_to_bf16(acc[ct][e + 2]) | (uint32_t)f32_to_bf16(acc[ct][e + 3]) << 16);
-            }
+        odd = store_row<D>(acc, 1.f / sum, there, o + i * w.row_q, d, h);
         if (lse && h == 0)
             lse[((size_t)b * w.heads + head) * w.n + i] = there ? (top + __builtin_log2f(sum)) * kWindowLn2 : -INFINITY;
     }
-    const uint64_t which = __ballot(odd && there);
+    const uint64_t which = __ballot(odd);
     for (uint32_t rows = (uint32_t)which | (uint32_t)(which >> 32); rows; rows &= rows - 1) {
         const int r = i0 + __ffs((int)rows) - 1;
         fwd_row_again<D>(w, q + r * w.row_q, k_rows, v_rows, o + r * w.row_q, r);
@@ -391,13 +399,6 @@ __device__ __forceinline__ void dkv_row_again(const Window &w, const bf16_t *k, 
         }
 }
 
-// Four values of a lane's result to a row in storage type.
-__device__ __forceinline__ void put4(bf16_t *at, float a, float b, float c, float e)
-{
-    *(uint2 *)at = make_uint2((uint32_t)f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16,
-                              (uint32_t)f32_to_bf16(c) | (uint32_t)f32_to_bf16(e) << 16);
-}
-
 // dQ, and D = <dO, o> of every row for the kernel below.
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q, const bf16_t *K, const bf16_t *V,
@@ -467,27 +468,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
         }
     }
     bool odd = false;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            acc[ct][e] *= i < end ? w.scale : 0.f;
-            if (32 * ct + place(e, h) < d) odd |= !(fabsf(acc[ct][e]) < INFINITY);
-        }
-    const bool there = i < end;
-    if (i < w.n)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int col = 32 * ct + place(e, h);
-                if (col < d) {
-                    bf16_t *to = dQ + at_q + i * w.row_q + col;
-                    if (there) put4(to, acc[ct][e], acc[ct][e + 1], acc[ct][e + 2], acc[ct][e + 3]);
-                    else *(uint2 *)to = make_uint2(0u, 0u);
-                }
-            }
-    const uint64_t which = __ballot(odd && there);
+    if (i < w.n) odd = store_row<D>(acc, w.scale, i < end, dQ + at_q + i * w.row_q, d, h);
+    const uint64_t which = __ballot(odd);
     for (uint32_t rows = (uint32_t)which | (uint32_t)(which >> 32); rows; rows &= rows - 1) {
         const int at = __ffs((int)rows) - 1, r = i0 + at;
         const int64_t row = at_q + r * w.row_q;
@@ -625,29 +607,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
             }
         return;
     }
-    const bool there = j < end;
     bool odd = false;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            acc_k[ct][e] *= w.scale;
-            if (32 * ct + place(e, h) < d) odd |= !(fabsf(acc_k[ct][e]) < INFINITY) || !(fabsf(acc_v[ct][e]) < INFINITY);
-        }
-    if (j < w.n)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int col = 32 * ct + place(e, h);
-                if (col >= d) continue;
-                bf16_t *to_k = dK + at_k + j * w.row_k + col, *to_v = dV + at_k + j * w.row_k + col;
-                if (there) {
-                    put4(to_k, acc_k[ct][e], acc_k[ct][e + 1], acc_k[ct][e + 2], acc_k[ct][e + 3]);
-                    put4(to_v, acc_v[ct][e], acc_v[ct][e + 1], acc_v[ct][e + 2], acc_v[ct][e + 3]);
-                } else *(uint2 *)to_k = *(uint2 *)to_v = make_uint2(0u, 0u);
-            }
-    const uint64_t bad = __ballot(odd && there);
+    if (j < w.n) {
+        odd = store_row<D>(acc_k, w.scale, j < end, dK + at_k + j * w.row_k, d, h);
+        odd |= store_row<D>(acc_v, 1.f, j < end, dV + at_k + j * w.row_k, d, h);
+    }
+    const uint64_t bad = __ballot(odd);
     for (uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32); rows; rows &= rows - 1) {
         const int r = j0 + __ffs((int)rows) - 1;
         const int64_t row = at_k + r * w.row_k;
