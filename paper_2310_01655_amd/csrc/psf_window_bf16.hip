@@ -132,13 +132,14 @@ __device__ __forceinline__ bool none_seen(const Window &w, int i0, int j0, int l
 
 // Which workgroup of the call (unit by unit, neighbouring rows side by side) workgroup `id` of the launch is.  The launch
 // deals its workgroups out to the 8 XCDs in turn; runs of 16 neighbours stay on one XCD, whose L2 serves the
-// tiles that they share, and the runs go round the XCDs, so that sequences of unequal length load all of them.
+// tiles that they share, and the runs go round the XCDs, one further every time round, so that neither sequences
+// of unequal length nor the long and the short rows of all units meet on the same ones.
 __device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t total)
 {
     constexpr uint32_t RUN = 16;
     if (id >= total / (8 * RUN) * (8 * RUN)) return id;
-    const uint32_t slot = id / 8;
-    return (slot / RUN * 8 + id % 8) * RUN + slot % RUN;
+    const uint32_t slot = id / 8, round = slot / RUN;
+    return (round * 8 + (id + round) % 8) * RUN + slot % RUN;
 }
 
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
