@@ -154,11 +154,13 @@ __device__ __forceinline__ uint32_t seen_by(const Window &w, int j, int i0, int 
     const int64_t reach = j < w.sinks ? (int64_t)end : (int64_t)j + w.window;
     return bits_below((reach < end ? (int)reach : end) - i0) & ~bits_below(j - i0);
 }
-// x where bit place(e, h) of `bits` >> 4 h is set, `other` elsewhere
+// x where bit place(E, h) of the row's bits is set, `other` elsewhere; bits_h: those bits >> 4 h.  (The bit as a mask, by an
+// instruction of its own: as a comparison and a select it takes five.)
 template <int E>
 __device__ __forceinline__ float pick(uint32_t bits_h, float x, uint32_t other)
 {
-    const uint32_t mask = (uint32_t)__builtin_amdgcn_sbfe((int)bits_h, 8 * (E / 4) + E % 4, 1);
+    uint32_t mask;
+    asm("v_bfe_i32 %0, %1, %2, 1" : "=v"(mask) : "v"(bits_h), "n"(8 * (E / 4) + E % 4));
     return __uint_as_float((__float_as_uint(x) & mask) | (other & ~mask));
 }
 
@@ -238,7 +240,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
     constexpr int KS = D / 16, CT = D / 32;
     using Tile = Staged<D>;
     __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 31, h = lane >> 5, d = w.d;
+    const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
     const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), unit = at_grid / groups;
     const int first = (int)(groups - 1 - (at_grid - unit * groups)) * kOwnWg;      // long rows first
     const int b = unit / w.heads, head = unit - b * w.heads;
@@ -410,7 +413,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
     constexpr int KS = D / 16, CT = D / 32;
     using Tile = Staged<D>;
     __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 31, h = lane >> 5, d = w.d;
+    const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
     const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), unit = at_grid / groups;
     const int first = (int)(groups - 1 - (at_grid - unit * groups)) * kOwnWg;
     const int b = unit / w.heads, head = unit - b * w.heads;
@@ -507,7 +511,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
     using Tile = Staged<D, TILE>;
     __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES + (V_IN_LDS ? kOwnWg * D * 2 : 0)];
     __shared__ float2 row_data[2][TILE];                  // L (in exponents of 2) and D of the tile's rows
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 31, h = lane >> 5, d = w.d;
+    const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
     const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), each = walks.each(), unit = at_grid / each;
     const int which = at_grid - unit * each, shared = walks.few * walks.parts;
     const int group = which < shared ? which / walks.parts : which - shared + walks.few;
