@@ -61,6 +61,13 @@ def causal_polysketch_attention(Q, K, V, G, p, r, b, local=psf.LOCAL_EXACT, per_
     return _CausalPolysketchAttention.apply(Q, K, V, G, desc)
 
 
+def _first_order_only():
+    # (what torch's once_differentiable does, at a tenth of its time: a backward pass with gradients enabled is one
+    # that is to be differentiated again)
+    if torch.is_grad_enabled():
+        raise RuntimeError("no second derivatives: call backward without create_graph")
+
+
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
@@ -71,8 +78,8 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
+        _first_order_only()
         x, weight, stats = ctx.saved_tensors
         dx, dweight, dbias = psf.psf_layer_norm_bwd(x, weight, stats, dy.contiguous(), want_bias=ctx.has_bias)
         return dx, dweight, dbias, None
@@ -95,8 +102,8 @@ class _CausalWindowAttention(torch.autograd.Function):
         return O
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dO):
+        _first_order_only()
         Q, K, V, lengths, O, lse = ctx.saved_tensors
         dQ, dK, dV = psf.psf_window_attn_bwd(ctx.desc, Q, K, V, O, lse, dO.contiguous(), lengths=lengths)
         return dQ, dK, dV, None, None

@@ -555,45 +555,47 @@ _CODES = {torch.float32: F32, torch.bfloat16: BF16}
 EVERYTHING = 2 ** 31 - 1             # a window that hides nothing
 
 
-def _place(tensors, stream):
+_AS_IT_IS = contextlib.nullcontext()
+
+
+def _place(stream, *tensors):
     """(context, device) of a call on these GPU tensors: with the context the device is the current one and `stream`
     the current stream."""
     device = None
-    for name, t in tensors:
+    for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
-            raise ValueError("%s must live on the GPU (no CPU path exists)" % name)
         if device is None:
+            if not t.is_cuda:
+                raise ValueError("tensors must live on the GPU (no CPU path exists)")
             device = t.device
         elif t.device != device:
-            raise ValueError("%s lives on %s, the call's other tensors on %s" % (name, t.device, device))
+            raise ValueError("all tensors of a call must live on one GPU, not on %s and %s" % (device, t.device))
     if stream is not None:
         if stream.device != device:
             raise ValueError("the stream belongs to %s, the tensors live on %s" % (stream.device, device))
         return torch.cuda.stream(stream), device
-    if device.index != torch._C._cuda_getDevice():
-        return torch.cuda.device(device), device
-    return contextlib.nullcontext(), device
+    return (_AS_IT_IS if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)), device
 
 
 def _ptr(t, dtype, shape, name):
     """Address of a contiguous tensor of this type and shape (None: no tensor)."""
     if t is None:
         return None
+    if t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    return t.data_ptr()
+    raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
 
 
 def _room(workspace, nbytes, device, name="workspace"):
-    """The caller's workspace, or one allocated for the current stream (None where nothing is needed)."""
+    """The caller's workspace, or one of nbytes() allocated for the current stream (None where nothing is needed)."""
     if workspace is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+        need = nbytes()
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
     if not workspace.is_cuda or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("%s must be a contiguous uint8 GPU tensor" % name)
     if workspace.device != device:
@@ -621,7 +623,7 @@ def psf_layer_norm_fwd(x, weight, bias=None, eps=1e-6, y=None, stats=None, want_
     """Layer normalisation over the last axis; returns y, or (y, stats) with want_stats or a stats tensor ([rows, 2]
     fp32: mean and inverse deviation, for psf_layer_norm_bwd)."""
     rows, width = _norm_rows(x)
-    where, device = _place((("x", x), ("weight", weight), ("bias", bias), ("y", y), ("stats", stats)), stream)
+    where, device = _place(stream, x, weight, bias, y, stats)
     with where:
         if y is None:
             y = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -637,13 +639,13 @@ def psf_layer_norm_fwd(x, weight, bias=None, eps=1e-6, y=None, stats=None, want_
 def psf_layer_norm_bwd(x, weight, stats, dy, want_bias=True, workspace=None, stream=None):
     """Gradients of psf_layer_norm_fwd: (dx, dweight, dbias), dbias None without want_bias."""
     rows, width = _norm_rows(x)
-    where, device = _place((("x", x), ("weight", weight), ("stats", stats), ("dy", dy)), stream)
+    where, device = _place(stream, x, weight, stats, dy)
     with where:
         dx = torch.empty_like(x, memory_format=torch.contiguous_format)
         dweight = torch.empty_like(weight)
         dbias = torch.empty_like(weight) if want_bias else None
         code = _CODES[x.dtype]
-        workspace = _room(workspace, lib().psf_layer_norm_bwd_workspace_bytes(rows, width, code), device)
+        workspace = _room(workspace, lambda: lib().psf_layer_norm_bwd_workspace_bytes(rows, width, code), device)
         _done(lib().psf_layer_norm_bwd(rows, width, code, _ptr(x, x.dtype, None, "x"), _ptr(weight, x.dtype, (width,), "weight"),
                                        _ptr(stats, torch.float32, (rows, 2), "stats"), _ptr(dy, x.dtype, x.shape, "dy"),
                                        dx.data_ptr(), dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
@@ -674,7 +676,7 @@ def psf_window_attn_fwd(desc, Q, K, V, lengths=None, O=None, lse=None, want_lse=
     _done(check_window_desc(desc), "psf_window_attn_fwd")
     shape_q, shape_k = _window_shapes(desc)
     dtype, rows = _torch_dtype(desc), (desc.batch, desc.heads, desc.n)
-    where, device = _place((("Q", Q), ("K", K), ("V", V), ("lengths", lengths), ("O", O), ("lse", lse)), stream)
+    where, device = _place(stream, Q, K, V, lengths, O, lse)
     with where:
         if O is None:
             O = torch.empty(shape_q, dtype=dtype, device=device)
@@ -696,9 +698,9 @@ def psf_window_attn_bwd(desc, Q, K, V, O, lse, dO, lengths=None, workspace=None,
     _done(check_window_desc(desc), "psf_window_attn_bwd")
     shape_q, shape_k = _window_shapes(desc)
     dtype = _torch_dtype(desc)
-    where, device = _place((("Q", Q), ("K", K), ("V", V), ("O", O), ("lse", lse), ("dO", dO), ("lengths", lengths)), stream)
+    where, device = _place(stream, Q, K, V, O, lse, dO, lengths)
     with where:
-        workspace = _room(workspace, window_bwd_workspace_bytes(desc), device)
+        workspace = _room(workspace, lambda: window_bwd_workspace_bytes(desc), device)
         dQ, dK, dV = (torch.empty(shape, dtype=dtype, device=device) for shape in (shape_q, shape_k, shape_k))
         _done(lib().psf_window_attn_bwd(
             ctypes.byref(desc), _ptr(Q, dtype, shape_q, "Q"), _ptr(K, dtype, shape_k, "K"), _ptr(V, dtype, shape_k, "V"),
@@ -734,13 +736,11 @@ def _cache_ptrs(desc, Kp, Vp, table, lengths):
 def psf_cache_append(desc, K, V, Kp, Vp, table, lengths, counts=None, stream=None):
     """Tokens t < counts[s] of K, V [seqs, kv_heads, n, d] to positions lengths[s] + t of the cache (counts None: all n).
     lengths are those before the call; the caller advances them."""
-    _done(check_cache_desc(desc), "psf_cache_append")
     if K.dim() != 4:
         raise ValueError("K must be [seqs, kv_heads, n, d]")
     n, dtype = K.shape[2], _torch_dtype(desc)
     shape = (desc.seqs, desc.kv_heads, n, desc.d)
-    where, _ = _place((("K", K), ("V", V), ("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("counts", counts)),
-                      stream)
+    where, _ = _place(stream, K, V, Kp, Vp, table, lengths, counts)
     with where:
         _done(lib().psf_cache_append(ctypes.byref(desc), n, _ptr(K, dtype, shape, "K"), _ptr(V, dtype, shape, "V"),
                                      *_cache_ptrs(desc, Kp, Vp, table, lengths),
@@ -750,10 +750,8 @@ def psf_cache_append(desc, K, V, Kp, Vp, table, lengths, counts=None, stream=Non
 def psf_cache_fork(desc, Kp, Vp, table, lengths, parents, children, fresh, stream=None):
     """Sequence children[k] becomes a copy of parents[k] that shares its full pages; a last page that is not full is copied
     to page fresh[k].  Writes the children's rows of table and lengths."""
-    _done(check_cache_desc(desc), "psf_cache_fork")
     forks = (parents.numel(),)
-    where, _ = _place((("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("parents", parents),
-                       ("children", children), ("fresh", fresh)), stream)
+    where, _ = _place(stream, Kp, Vp, table, lengths, parents, children, fresh)
     with where:
         _done(lib().psf_cache_fork(ctypes.byref(desc), forks[0], *_cache_ptrs(desc, Kp, Vp, table, lengths),
                                    *(_ptr(t, torch.int32, forks, name) for t, name in
@@ -768,9 +766,7 @@ def alloc_compact_workspace(desc, device="cuda"):
 def psf_cache_compact(desc, Kp, Vp, table, lengths, new_table=None, live=None, workspace=None, stream=None):
     """Moves the pages in use to the front of the pools; returns (new_table, live): the table with the new places and the
     number of pages in use (int32 [1] on the GPU; the pages from it on are free)."""
-    _done(check_cache_desc(desc), "psf_cache_compact")
-    where, device = _place((("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("new_table", new_table),
-                            ("live", live)), stream)
+    where, device = _place(stream, Kp, Vp, table, lengths, new_table, live)
     with where:
         if new_table is None:
             new_table = torch.empty_like(table)
@@ -778,7 +774,7 @@ def psf_cache_compact(desc, Kp, Vp, table, lengths, new_table=None, live=None, w
             raise ValueError("new_table must not be table")
         if live is None:
             live = torch.empty(1, dtype=torch.int32, device=device)
-        workspace = _room(workspace, lib().psf_cache_compact_workspace_bytes(ctypes.byref(desc)), device)
+        workspace = _room(workspace, lambda: lib().psf_cache_compact_workspace_bytes(ctypes.byref(desc)), device)
         _done(lib().psf_cache_compact(ctypes.byref(desc), *_cache_ptrs(desc, Kp, Vp, table, lengths),
                                       _ptr(new_table, torch.int32, (desc.seqs, desc.cols), "new_table"),
                                       _ptr(live, torch.int32, (1,), "live"), *_room_args(workspace), _stream_ptr(None)),
@@ -797,16 +793,15 @@ def alloc_paged_workspace(desc, heads, device="cuda"):
 def psf_paged_attn(desc, q, Kp, Vp, table, lengths, window=None, sinks=0, scale=None, o=None, workspace=None, stream=None):
     """Attention of one new token a sequence (q [seqs, heads, 1, d], at position lengths - 1, its key and value in the
     cache already) over the paged cache; returns o of q's shape.  window None: every position."""
-    _done(check_cache_desc(desc), "psf_paged_attn")
     if q.dim() != 4:
         raise ValueError("q must be [seqs, heads, 1, d]")
     heads, dtype = q.shape[1], _torch_dtype(desc)
     shape = (desc.seqs, heads, 1, desc.d)
-    where, device = _place((("q", q), ("Kp", Kp), ("Vp", Vp), ("table", table), ("lengths", lengths), ("o", o)), stream)
+    where, device = _place(stream, q, Kp, Vp, table, lengths, o)
     with where:
         if o is None:
             o = torch.empty(shape, dtype=dtype, device=device)
-        workspace = _room(workspace, paged_workspace_bytes(desc, heads), device)
+        workspace = _room(workspace, lambda: paged_workspace_bytes(desc, heads), device)
         _done(lib().psf_paged_attn(ctypes.byref(desc), heads, EVERYTHING if window is None else window, sinks,
                                    desc.d ** -0.5 if scale is None else scale, _ptr(q, dtype, shape, "q"),
                                    *_cache_ptrs(desc, Kp, Vp, table, lengths), _ptr(o, dtype, shape, "o"),

@@ -111,75 +111,96 @@ __global__ __launch_bounds__(kCacheThreads) void cache_fork_kernel(u4 *Kp, u4 *V
 }
 
 // Which pages move: one workgroup, a bit for every page in LDS.  `live` pages are in use; the k-th free page
-// below that number takes the k-th used page from it on.  moves[k] = {from, to}, place[from] = to.
-constexpr int kPlanThreads = 1024;
+// below that number, to[k], takes the k-th used page from it on, from[k]; place[from[k]] = k.  Bound by the latency of its steps
+// (lengths, table, two scans), so the table's entries are loaded four a lane and row at a time.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(const int32_t *table, const int32_t *lengths, Cache c,
-                                                                  int32_t *live, int32_t *n_moves, int2 *moves, int32_t *place)
+                                                                  int32_t *live, int32_t *n_moves, int32_t *from, int32_t *to,
+                                                                  int32_t *place)
 {
+    constexpr int AHEAD = 4, ROWS = 1024;                  // ROWS: lengths held in LDS at a time
     __shared__ uint32_t used[PSF_CACHE_MAX_PAGES / 32];
-    __shared__ int sums[kPlanThreads / 64];
+    __shared__ int2 sums[kPlanWaves];
+    __shared__ int needs[ROWS];
     const int words = (c.pages + 31) / 32, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int i = tid; i < words; i += kPlanThreads) used[i] = 0u;
-    __syncthreads();
-    for (int seq = wave; seq < c.seqs; seq += kPlanThreads / 64) {
-        const int length = lengths[seq];
-        const int need = length <= 0 ? 0 : (length - 1) / c.page + 1, most = need < c.cols ? need : c.cols;
-        for (int i = lane; i < most; i += 64) {
-            const int p = page_of(table + (size_t)seq * c.cols, i, c.cols, c.pages);
-            if (p >= 0) atomicOr(&used[p >> 5], 1u << (p & 31));
+    for (int base = 0; base < c.seqs; base += ROWS) {
+        __syncthreads();
+        if (base + tid < c.seqs) {
+            const int length = lengths[base + tid], need = length <= 0 ? 0 : (length - 1) / c.page + 1;
+            needs[tid] = need < c.cols ? need : c.cols;
+        }
+        __syncthreads();
+        const int rows = c.seqs - base < ROWS ? c.seqs - base : ROWS;
+        for (int r = wave; r < rows; r += kPlanWaves) {
+            const int32_t *row = table + (size_t)(base + r) * c.cols;
+            const int need = needs[r];
+            for (int i = lane; i < need; i += 64 * AHEAD) {
+                int p[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) p[k] = i + 64 * k < need ? row[i + 64 * k] : -1;
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+                    if ((unsigned)p[k] < (unsigned)c.pages) atomicOr(&used[p[k] >> 5], 1u << (p[k] & 31));
+            }
         }
     }
     __syncthreads();
-    // words of a thread: [first, last); total and the number of used pages before its own
+    // words of a thread: [first, last); sums over the threads before it, and over all
     const int each = (words + kPlanThreads - 1) / kPlanThreads, first = tid * each < words ? tid * each : words,
               last = first + each < words ? first + each : words;
-    auto before = [&](int mine, int &total) {
-        int run = mine;
+    auto before = [&](int2 mine, int2 &total) {
+        int2 run = mine;
 #pragma unroll
         for (int k = 1; k < 64; k <<= 1) {
-            const int up = __shfl_up(run, k);
-            if (lane >= k) run += up;
+            const int x = __shfl_up(run.x, k), y = __shfl_up(run.y, k);
+            if (lane >= k) {
+                run.x += x;
+                run.y += y;
+            }
         }
         __syncthreads();
         if (lane == 63) sums[wave] = run;
         __syncthreads();
-        int base = 0;
-        total = 0;
-        for (int k = 0; k < kPlanThreads / 64; ++k) {
-            if (k < wave) base += sums[k];
-            total += sums[k];
+        int2 base = make_int2(0, 0);
+        total = make_int2(0, 0);
+#pragma unroll
+        for (int k = 0; k < kPlanWaves; ++k) {
+            const int2 s = sums[k];
+            if (k < wave) {
+                base.x += s.x;
+                base.y += s.y;
+            }
+            total.x += s.x;
+            total.y += s.y;
         }
-        return base + run - mine;
+        return make_int2(base.x + run.x - mine.x, base.y + run.y - mine.y);
     };
-    int mine = 0, total = 0, unused = 0;
-    for (int i = first; i < last; ++i) mine += __popc(used[i]);
+    int2 mine = make_int2(0, 0), total, moving;
+    for (int i = first; i < last; ++i) mine.x += __popc(used[i]);
     (void)before(mine, total);
-    // bits of word i that stand for pages below / from `total` on
+    // bits of word i that stand for pages below `live`
     auto below = [&](int i) -> uint32_t {
-        const int left = total - 32 * i;
+        const int left = total.x - 32 * i;
         return left <= 0 ? 0u : left >= 32 ? 0xffffffffu : (1u << left) - 1u;
     };
-    int holes = 0, movers = 0;
+    mine = make_int2(0, 0);
     for (int i = first; i < last; ++i) {
-        holes += __popc(~used[i] & below(i));
-        movers += __popc(used[i] & ~below(i));
+        mine.x += __popc(~used[i] & below(i));
+        mine.y += __popc(used[i] & ~below(i));
     }
-    int at = before(holes, unused);
-    for (int i = first; i < last; ++i)
-        for (uint32_t bits = ~used[i] & below(i); bits; bits &= bits - 1) moves[at++].y = 32 * i + __ffs(bits) - 1;
-    int all = 0;
-    at = before(movers, all);                               // (its barriers order the holes' writes before the reads below)
-    __threadfence_block();
-    __syncthreads();
-    for (int i = first; i < last; ++i)
+    int2 at = before(mine, moving);
+    for (int i = first; i < last; ++i) {
+        for (uint32_t bits = ~used[i] & below(i); bits; bits &= bits - 1) to[at.x++] = 32 * i + __ffs(bits) - 1;
         for (uint32_t bits = used[i] & ~below(i); bits; bits &= bits - 1) {
-            const int from = 32 * i + __ffs(bits) - 1;
-            place[from] = moves[at].y;
-            moves[at++].x = from;
+            const int p = 32 * i + __ffs(bits) - 1;
+            place[p] = at.y;
+            from[at.y++] = p;
         }
+    }
     if (tid == 0) {
-        *live = total;
-        *n_moves = all;
+        *live = total.x;
+        *n_moves = moving.y;
     }
 }
 
@@ -187,26 +208,25 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(const int32_t 
 __global__ __launch_bounds__(kCacheThreads) void cache_move_kernel(u4 *Kp, u4 *Vp, const int32_t *table, const int32_t *lengths,
                                                                    int32_t *new_table, Cache c, size_t pieces, uint32_t parts,
                                                                    const int32_t *live, const int32_t *n_moves,
-                                                                   const int2 *moves, const int32_t *place, FastDiv cols,
-                                                                   FastDiv page)
+                                                                   const int32_t *from, const int32_t *to,
+                                                                   const int32_t *place, FastDiv cols, FastDiv page)
 {
     const int most = *live;
     const uint32_t entries = (uint32_t)c.seqs * c.cols;
     for (uint32_t i = blockIdx.x * kCacheThreads + threadIdx.x; i < entries; i += gridDim.x * kCacheThreads) {
         const uint32_t seq = cols.div(i), col = i - seq * cols.by;
         const int length = lengths[seq];
-        int to = -1;
+        int now = -1;
         if (length > 0 && col <= page.div((uint32_t)length - 1)) {
             const int p = table[i];
-            if ((unsigned)p < (unsigned)c.pages) to = p < most ? p : place[p];
+            if ((unsigned)p < (unsigned)c.pages) now = p < most ? p : to[place[p]];
         }
-        new_table[i] = to;
+        new_table[i] = now;
     }
     const uint64_t units = (uint64_t)*n_moves * parts;
     for (uint64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const uint32_t k = (uint32_t)(u / parts), part = (uint32_t)(u - (uint64_t)k * parts);
-        const int2 m = moves[k];
-        copy_page(Kp, Vp, pieces, m.x, m.y, part, parts);
+        copy_page(Kp, Vp, pieces, from[k], to[k], part, parts);
     }
 }
 
@@ -280,7 +300,7 @@ size_t psf_cache_compact_workspace_bytes(const psf_cache_desc *desc)
 {
     Cache c;
     if (make_cache(desc, &c) != PSF_OK) return 0;
-    return align_up(64 + (size_t)c.pages * (sizeof(int2) + sizeof(int32_t)), 256);
+    return align_up(64 + (size_t)c.pages * 3 * sizeof(int32_t), 256);
 }
 
 psf_status psf_cache_compact(const psf_cache_desc *desc, void *Kp, void *Vp, const int32_t *table, const int32_t *lengths,
@@ -294,10 +314,9 @@ psf_status psf_cache_compact(const psf_cache_desc *desc, void *Kp, void *Vp, con
     if (((uintptr_t)workspace & 255u) != 0) return PSF_ERR_WORKSPACE;
     if (!aligned16({Kp, Vp})) return PSF_ERR_ALIGNMENT;
     int32_t *n_moves = (int32_t *)workspace;
-    int2 *moves = (int2 *)((char *)workspace + 64);
-    int32_t *place = (int32_t *)(moves + c.pages);
+    int32_t *from = n_moves + 16, *to = from + c.pages, *place = to + c.pages;
     hipStream_t s = (hipStream_t)hip_stream;
-    hipLaunchKernelGGL(cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, table, lengths, c, live, n_moves, moves, place);
+    hipLaunchKernelGGL(cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, table, lengths, c, live, n_moves, from, to, place);
     PSF_LAUNCH_CHECK();
     const size_t pieces = c.page_bytes() / 16;
     const uint32_t parts = page_parts(pieces);
@@ -305,7 +324,7 @@ psf_status psf_cache_compact(const psf_cache_desc *desc, void *Kp, void *Vp, con
     const uint64_t entries = ((uint64_t)c.seqs * c.cols + kCacheThreads - 1) / kCacheThreads;
     const uint64_t want = most > entries ? most : entries;
     hipLaunchKernelGGL(cache_move_kernel, dim3((uint32_t)(want < 2048 ? want : 2048)), dim3(kCacheThreads), 0, s, (u4 *)Kp,
-                       (u4 *)Vp, table, lengths, new_table, c, pieces, parts, live, n_moves, moves, place, fast_div(c.cols),
+                       (u4 *)Vp, table, lengths, new_table, c, pieces, parts, live, n_moves, from, to, place, fast_div(c.cols),
                        fast_div(c.page));
     PSF_LAUNCH_CHECK();
     return PSF_OK;
