@@ -58,6 +58,60 @@ struct KeyTiles {
     __device__ __forceinline__ int at(int k) const { return k < few ? k : window_first + k - few; }
 };
 
+// How the walks of the key side are shared out.  A workgroup of `own` keys walks the tiles of queries that see one of them, head
+// after head of the group.  The first `few` workgroups of a unit hold the tokens that every later row sees; their
+// walks are `parts` times as long as the others' and go to as many workgroups, whose shares a second kernel adds in order.
+struct KeyWalks {
+    int few, parts, groups;                // groups: workgroups of `own` keys of a unit
+    __host__ __device__ int each() const { return groups - few + few * parts; }
+};
+// Workgroup `which` of a unit: its group of keys and its part of their walk.
+struct KeyWalk {
+    int group, part, parts;
+    __device__ __forceinline__ KeyWalk(const KeyWalks &k, int which)
+    {
+        const int shared = k.few * k.parts;
+        group = which < shared ? which / k.parts : which - shared + k.few;
+        part = which < shared ? which % k.parts : 0;
+        parts = which < shared ? k.parts : 1;
+    }
+};
+// Queries that see one of the keys [first, first + own): tiles [tile0, tile0 + count) of `size` rows.
+struct QueryTiles {
+    int tile0, count;
+    __device__ __forceinline__ QueryTiles(const Window &w, int first, int end, int own, int size)
+    {
+        const int64_t reach = first < w.sinks ? (int64_t)end - 1 : (int64_t)first + own - 1 + w.window - 1;
+        const int last = reach < end ? (int)reach : end - 1;
+        tile0 = first / size;
+        count = last / size + 1 - tile0;
+    }
+};
+// Long walks of the first tokens are cut to the length of the others', but into no more workgroups than a few for every
+// CU in all (their shares lie in memory: 1 KB for a key at d = 128).
+inline KeyWalks key_walks(const Window &w, int own, int size)
+{
+    KeyWalks k;
+    k.groups = (w.n + own - 1) / own;
+    k.few = 0;
+    k.parts = 1;
+    const int holding = (w.sinks + own - 1) / own;         // (sinks is at most n)
+    if (holding == 0) return k;
+    const int longest = (w.n + size - 1) / size, other = (w.window + own - 2) / size + 1;
+    const int64_t most = 1024 / ((int64_t)holding * w.batch * w.kv_heads);
+    int64_t parts = (longest + other - 1) / other;
+    if (parts > most) parts = most;
+    if (parts <= 1) return k;
+    k.few = holding;
+    k.parts = (int)parts;
+    return k;
+}
+// Shares: [unit][group][part][dK, dV][own][d] floats.
+inline size_t key_walks_room(const Window &w, const KeyWalks &k, int own)
+{
+    return k.parts == 1 ? 0 : (size_t)w.batch * w.kv_heads * k.few * k.parts * 2 * own * w.d * sizeof(float);
+}
+
 psf_status window_bf16_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s);
 psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s);
 size_t window_bf16_room(const Window &w);              // bytes of WindowPtrs::room

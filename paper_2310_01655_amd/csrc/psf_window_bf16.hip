@@ -482,25 +482,6 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
     }
 }
 
-// How the walks of the key side are shared out.  A workgroup of 128 keys walks the tiles of 64 queries that see one of them, head
-// after head of the group.  The first `few` workgroups of a unit hold the tokens that every later row sees; their
-// walks are `parts` times as long as the others' and go to as many workgroups, whose shares a second kernel adds.
-struct KeyWalks {
-    int few, parts, groups;                // groups: workgroups of 128 keys of a unit
-    __host__ __device__ int each() const { return groups - few + few * parts; }
-};
-// queries that see one of the keys from `first` on (a workgroup's): tiles [tile0, tile0 + count)
-struct QueryTiles {
-    int tile0, count;
-    __host__ __device__ QueryTiles(const Window &w, int first, int end, int size)
-    {
-        const int64_t reach = first < w.sinks ? (int64_t)end - 1 : (int64_t)first + kOwnWg - 1 + w.window - 1;
-        const int last = reach < end ? (int)reach : end - 1;
-        tile0 = first / size;
-        count = last / size + 1 - tile0;
-    }
-};
-
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
     const bf16_t *Q, const bf16_t *K, const bf16_t *V, const int32_t *lengths, const float *lse, const bf16_t *dO,
@@ -514,9 +495,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
     const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
     const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), each = walks.each(), unit = at_grid / each;
-    const int which = at_grid - unit * each, shared = walks.few * walks.parts;
-    const int group = which < shared ? which / walks.parts : which - shared + walks.few;
-    const int part = which < shared ? which % walks.parts : 0, parts = which < shared ? walks.parts : 1;
+    const KeyWalk walk(walks, at_grid - unit * each);
+    const int group = walk.group, part = walk.part, parts = walk.parts;
     const int first = group * kOwnWg;
     const int b = unit / w.kv_heads, kv = unit - b * w.kv_heads;
     const int end = window_end(lengths, b, w.n), j0 = first + kOwn * wave, j = j0 + x;
@@ -527,7 +507,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc_k[ct] = acc_v[ct] = f32x16{0};
     if (first < end) {
-        const QueryTiles tiles(w, first, end, TILE);
+        const QueryTiles tiles(w, first, end, kOwnWg, TILE);
         const int total = tiles.count * w.group, begin = (int)((int64_t)total * part / parts),
                   stop = (int)((int64_t)total * (part + 1) / parts);
         const Tile stage(lds, d);
@@ -664,25 +644,7 @@ __global__ __launch_bounds__(kThreads) void window_share_kernel(const bf16_t *Q,
     if (__any(odd)) dkv_row_again<D>(w, K + to, V + to, Q + at_q, dO + at_q, lse + at_rows, delta + at_rows, end, dK + to, dV + to, j);
 }
 
-// Long walks of the first tokens are cut to the length of the others', but into no more workgroups than a few for every
-// CU in all (their shares lie in memory: 128 KB each at d = 128).
-KeyWalks key_walks(const Window &w)
-{
-    KeyWalks k;
-    k.groups = (w.n + kOwnWg - 1) / kOwnWg;
-    k.few = 0;
-    k.parts = 1;
-    const int sinks = w.sinks < w.n ? w.sinks : w.n, holding = (sinks + kOwnWg - 1) / kOwnWg;
-    if (holding == 0) return k;
-    const int longest = (w.n + kTile - 1) / kTile, other = (w.window + kOwnWg - 2) / kTile + 1;
-    const int64_t most = 1024 / ((int64_t)holding * w.batch * w.kv_heads);
-    int64_t parts = (longest + other - 1) / other;
-    if (parts > most) parts = most;
-    if (parts <= 1) return k;
-    k.few = holding;
-    k.parts = (int)parts;
-    return k;
-}
+KeyWalks walks_of(const Window &w) { return key_walks(w, kOwnWg, w.d <= 64 ? 64 : 32); }
 
 }  // namespace
 
@@ -701,8 +663,7 @@ psf_status window_bf16_fwd(const Window &w, const WindowPtrs &p, void *O, float 
 
 size_t window_bf16_room(const Window &w)
 {
-    const KeyWalks k = key_walks(w);
-    return k.parts == 1 ? 0 : (size_t)w.batch * w.kv_heads * k.few * k.parts * 2 * kOwnWg * w.d * sizeof(float);
+    return key_walks_room(w, walks_of(w), kOwnWg);
 }
 
 psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
@@ -716,7 +677,7 @@ psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
         hipLaunchKernelGGL((window_dq_kernel<D>), dim3(groups * w.batch * w.heads), dim3(kThreads), 0, s, Q, K, V, p.lengths, O, p.lse,
                            dO, dQ, p.delta, w, groups);
         PSF_LAUNCH_CHECK();
-        const KeyWalks walks = key_walks(w);
+        const KeyWalks walks = walks_of(w);
         const uint32_t units = w.batch * w.kv_heads;
         hipLaunchKernelGGL((window_dkv_kernel<D>), dim3(units * walks.each()), dim3(kThreads), 0, s, Q, K, V, p.lengths, p.lse, dO,
                            p.delta, dK, dV, p.room, w, walks);

@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const 
 template <int NT, typename S>
 __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const S *K, const S *V, const S *dO,
                                                                const int32_t *lengths, const float *lse, const float *delta,
-                                                               S *dK, S *dV, Window w)
+                                                               S *dK, S *dV, float *room, Window w, KeyWalks walks)
 {
     constexpr int KS = NT / 2, P = parts_of<S>();
     using Tiles = TilePair<NT, S>;
@@ -219,8 +219,9 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
     __shared__ int odd_seen;
     if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const KeyWalk walk(walks, blockIdx.x);
     const int b = blockIdx.y / w.kv_heads, kv = blockIdx.y % w.kv_heads, d = w.d;
-    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, j = first + 16 * wave + li;
+    const int end = window_end(lengths, b, w.n), first = walk.group * kRows, own_at = 16 * wave + li, j = first + own_at;
     const int64_t at_k = b * w.batch_k + kv * w.head_k;
     f4 acc_k[NT], acc_v[NT];
     clear(acc_k);
@@ -235,10 +236,9 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
             row.parts(own, d, g);
             row_v.parts(own_v, d, g);
         }
-        // queries that see one of the keys: [first, last]
-        const int64_t reach = first < w.sinks ? end - 1 : (int64_t)first + kRows - 1 + w.window - 1;
-        const int last = reach < end ? (int)reach : end - 1;
-        const int tile0 = first / kTile, per = last / kTile + 1 - tile0, total = per * w.group;
+        const QueryTiles tiles(w, first, end, kRows, kTile);
+        const int tile0 = tiles.tile0, per = tiles.count, total = per * w.group;
+        const int begin = (int)((int64_t)total * walk.part / walk.parts), stop = (int)((int64_t)total * (walk.part + 1) / walk.parts);
         Tiles next;
         float next_l = 0.f, next_d = 0.f;
         auto load = [&](int k) {
@@ -251,8 +251,8 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
                 next_d = delta[row];
             }
         };
-        load(0);
-        for (int k = 0; k < total; ++k) {
+        if (begin < stop) load(begin);
+        for (int k = begin; k < stop; ++k) {
             const int i0 = (tile0 + k % per) * kTile;
             __syncthreads();
             if (threadIdx.x < kTile) {
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
                 rows_d[threadIdx.x] = next_d;
             }
             const int odd = next.store(tq, tg, end - i0, d, &odd_seen);
-            if (k + 1 < total) load(k + 1);
+            if (k + 1 < stop) load(k + 1);
             f4 s[2], t[2];
             score_parts<2, KS, P, P>(tq, Tiles::PLANE, Tiles::PITCH, 0, own, lane, s);
             score_parts<2, KS, P, P>(tg, Tiles::PLANE, Tiles::PITCH, 0, own_v, lane, t);
@@ -278,11 +278,40 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
         }
     }
     if (j >= w.n) return;
+    if (walk.parts > 1) {
+        float *to = room + (((size_t)blockIdx.y * walks.few + walk.group) * walk.parts + walk.part) * 2 * kRows * d + (size_t)own_at * d;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            store_piece(to, 16 * t + 4 * g, d, 1, acc_k[t]);
+            store_piece(to + (size_t)kRows * d, 16 * t + 4 * g, d, 1, acc_v[t]);
+        }
+        return;
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         store_piece(dK + at_k + j * w.row_k, 16 * t + 4 * g, d, 1, acc_k[t] * w.scale);
         store_piece(dV + at_k + j * w.row_k, 16 * t + 4 * g, d, 1, acc_v[t]);
     }
+}
+
+// The shares of the first tokens' gradients added in order: a thread four columns of a row.
+template <typename S>
+__global__ __launch_bounds__(256) void window_parts_share_kernel(S *dK, S *dV, const float *room, Window w, KeyWalks walks)
+{
+    const int pieces = w.d / 4, rows = walks.few * kRows;
+    const int at = blockIdx.x * 256 + threadIdx.x, row = at / pieces, c = 4 * (at - row * pieces);
+    const int b = blockIdx.y / w.kv_heads, kv = blockIdx.y % w.kv_heads;
+    if (row >= rows || row >= w.n) return;
+    const float *from = room + ((size_t)blockIdx.y * walks.few + row / kRows) * walks.parts * 2 * kRows * w.d + (size_t)(row % kRows) * w.d + c;
+    f4 k = {0.f, 0.f, 0.f, 0.f}, v = k;
+#pragma unroll 4
+    for (int p = 0; p < walks.parts; ++p) {
+        k += load4(from + (size_t)p * 2 * kRows * w.d);
+        v += load4(from + ((size_t)p * 2 + 1) * kRows * w.d);
+    }
+    const int64_t to = b * w.batch_k + kv * w.head_k + row * w.row_k + c;
+    store4(dK + to, k * w.scale);
+    store4(dV + to, v);
 }
 
 template <class F>
@@ -305,7 +334,7 @@ psf_status window_parts_fwd(const Window &w, const WindowPtrs &p, void *O, float
     });
 }
 
-size_t window_parts_room(const Window &) { return 0; }
+size_t window_parts_room(const Window &w) { return key_walks_room(w, key_walks(w, kRows, kTile), kRows); }
 
 psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
 {
@@ -316,8 +345,15 @@ psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
         hipLaunchKernelGGL((window_parts_dq_kernel<NT, S>), dim3(tiles, w.batch * w.heads), dim3(256), 0, s, (const S *)p.Q,
                            (const S *)p.K, (const S *)p.V, (const S *)p.O, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dQ, w);
         PSF_LAUNCH_CHECK();
-        hipLaunchKernelGGL((window_parts_dkv_kernel<NT, S>), dim3(tiles, w.batch * w.kv_heads), dim3(256), 0, s, (const S *)p.Q,
-                           (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dK, (S *)p.dV, w);
+        const KeyWalks walks = key_walks(w, kRows, kTile);
+        const unsigned units = w.batch * w.kv_heads;
+        hipLaunchKernelGGL((window_parts_dkv_kernel<NT, S>), dim3(walks.each(), units), dim3(256), 0, s, (const S *)p.Q,
+                           (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dK, (S *)p.dV,
+                           p.room, w, walks);
+        PSF_LAUNCH_CHECK();
+        if (walks.parts == 1) return PSF_OK;
+        hipLaunchKernelGGL((window_parts_share_kernel<S>), dim3((walks.few * kRows * (w.d / 4) + 255) / 256, units), dim3(256), 0, s,
+                           (S *)p.dK, (S *)p.dV, p.room, w, walks);
         PSF_LAUNCH_CHECK();
         return PSF_OK;
     });
