@@ -106,7 +106,7 @@ __device__ __forceinline__ void wait_vmem_le()
 // (us a call, with and without): 60 units of 4096, no mask 97, 87; gradients of 96 units of 4096, d = 64 838, 778, 16 units of
 // 16384, d = 128 2238, 2048; causal, 24 units of 32768 807, 768.
 template <int D>
-__device__ __forceinline__ int row_swz(int j)
+__device__ __forceinline__ constexpr int row_swz(int j)
 {
     static_assert(D == 64 || D == 128, "8 or 16 pieces");
     if constexpr (D == 64) return ((j & 3) << 1) ^ ((j >> 2) & 1) ^ ((j >> 2) & 2);

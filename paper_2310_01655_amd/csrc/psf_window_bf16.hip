@@ -48,27 +48,33 @@ struct Staged {
 };
 
 // This lane's reads of a staged tile: operand A along the rows (row 32 t + lane % 32, piece 2 s + lane / 32), and
-// transposed (columns 32 ct + lane % 32, rows 16 s + {4 h .. 4 h + 3, 8 + 4 h ..}, h = lane / 32).
+// transposed (columns 32 ct + lane % 32, rows 16 s + {4 h .. 4 h + 3, 8 + 4 h ..}, h = lane / 32).  A piece's place in
+// its row is its number with bits of the row's flipped, so all places of a tile come from one address by flips of
+// constant bits: two registers a tile instead of one for every place.
 template <int D>
 struct Reads {
-    uint32_t along[D / 16], turned[2][D / 32];
+    uint32_t along, turned;                                // LDS addresses (tiles start at multiples of 256 bytes)
     __device__ __forceinline__ Reads(int lane)
     {
         const int x = lane & 31, h = lane >> 5;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) along[s] = (uint32_t)((x * (D / 8) + ((2 * s + h) ^ row_swz<D>(x))) * 16);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int ct = 0; ct < D / 32; ++ct) turned[e][ct] = row_turned_offset<D>(lane, 8 * e + 4 * h, ct);
+        along = (uint32_t)((x * (D / 8) + (h ^ row_swz<D>(x))) * 16);
+        turned = row_turned_offset<D>(lane, 4 * h, 0);
     }
-    __device__ __forceinline__ bf16x8 row(const unsigned char *tile, int t, int s) const
+    __device__ __forceinline__ Reads(const Reads &in_tile, uint32_t tile) : along(in_tile.along + tile), turned(in_tile.turned + tile) {}
+    __device__ __forceinline__ bf16x8 row(int t, int s) const
     {
-        return *(const bf16x8 *)(tile + along[s] + t * (32 * D * 2));
+        return *(__attribute__((address_space(3))) const bf16x8 *)(uintptr_t)((along ^ (32 * s)) + t * (32 * D * 2));
     }
-    __device__ __forceinline__ bf16x8 column(const unsigned char *tile, int ct, int s) const
+    __device__ __forceinline__ bf16x8 column(int ct, int s) const
     {
-        return read_turned(tile + turned[0][ct] + s * (16 * D * 2), tile + turned[1][ct] + s * (16 * D * 2));
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        typedef __attribute__((address_space(3))) s16x4 *at;
+        constexpr uint32_t EIGHT = (row_swz<D>(8) ^ row_swz<D>(0)) * 16;       // rows 8 further: their flips
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(uintptr_t)((turned ^ (64 * ct)) + s * (16 * D * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (at)(uintptr_t)((turned ^ (64 * ct) ^ EIGHT) + s * (16 * D * 2) + 8 * D * 2));
+        return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 
@@ -95,26 +101,40 @@ __device__ __forceinline__ float other_half(float x, bool take_max)
     return take_max ? fmaxf(a, b) : a + b;
 }
 
+// The order of a block's LDS reads and products, for a loop of PRODUCTS products that take READS reads each: AHEAD products'
+// reads before the first one, then product and reads in turn.  Left alone the compiler puts a read right before
+// its product and waits for it there, 100 cycles for a product of 32.
+template <int PRODUCTS, int READS, int AHEAD>
+__device__ __forceinline__ void read_ahead()
+{
+    constexpr int DS_READ = 0x100, MFMA = 0x8;
+    __builtin_amdgcn_sched_group_barrier(DS_READ, READS * AHEAD, 0);
+    static_for<PRODUCTS>([&](auto k) {
+        __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+        if constexpr (decltype(k)::value + AHEAD < PRODUCTS) __builtin_amdgcn_sched_group_barrier(DS_READ, READS, 0);
+    });
+}
+
 // scores of a tile's 32 rows (half t) with the wave's own rows
 template <int D>
-__device__ __forceinline__ f32x16 scores(const Reads<D> &at, const unsigned char *tile, int t, const bf16x8 (&own)[D / 16])
+__device__ __forceinline__ f32x16 scores(const Reads<D> &tile, int t, const bf16x8 (&own)[D / 16])
 {
     f32x16 c = {0};
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) c = mfma32(at.row(tile, t, s), own[s], c);
+    for (int s = 0; s < D / 16; ++s) c = mfma32(tile.row(t, s), own[s], c);
     return c;
 }
 // acc += tile^T w: the tile's rows 32 t .. with weights w (as results hold them), columns of the tile as rows of acc
-template <int D>
-__device__ __forceinline__ void add_turned(const Reads<D> &at, const unsigned char *tile, int t, const f32x16 &w,
-                                           f32x16 (&acc)[D / 32])
+template <int D, int AHEAD = 3>
+__device__ __forceinline__ void add_turned(const Reads<D> &tile, int t, const f32x16 &w, f32x16 (&acc)[D / 32])
 {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const bf16x8 b = cvt8_from16(w, 8 * s);
 #pragma unroll
-        for (int ct = 0; ct < D / 32; ++ct) acc[ct] = mfma32(at.column(tile, ct, 2 * t + s), b, acc[ct]);
+        for (int ct = 0; ct < D / 32; ++ct) acc[ct] = mfma32(tile.column(ct, 2 * t + s), b, acc[ct]);
     }
+    read_ahead<2 * (D / 32), 2, AHEAD>();
 }
 
 // place in its 32 rows of element e of a result
@@ -131,12 +151,14 @@ __device__ __forceinline__ bool none_seen(const Window &w, int i0, int j0, int l
 }
 
 // Which workgroup of the call (unit by unit, neighbouring rows side by side) workgroup `id` of the launch is.  The launch
-// deals its workgroups out to the 8 XCDs in turn; runs of 16 neighbours stay on one XCD, whose L2 serves the
+// deals its workgroups out to the 8 XCDs in turn; runs of RUN neighbours stay on one XCD, whose L2 serves the
 // tiles that they share, and the runs go round the XCDs, one further every time round, so that neither sequences
-// of unequal length nor the long and the short rows of all units meet on the same ones.
+// of unequal length nor the long and the short rows of all units meet on the same ones.  16 for the query side (8 x 12 x
+// 4096, window 1024, lengths from 0 to 4096: forward 86 us, with runs of 2 95), 2 for the key side, whose walks are longer and
+// fewer at a time (172 us, with runs of 16 187).
+template <uint32_t RUN>
 __device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t total)
 {
-    constexpr uint32_t RUN = 16;
     if (id >= total / (8 * RUN) * (8 * RUN)) return id;
     const uint32_t slot = id / 8, round = slot / RUN;
     return (round * 8 + (id + round) % 8) * RUN + slot % RUN;
@@ -165,71 +187,114 @@ __device__ __forceinline__ float pick(uint32_t bits_h, float x, uint32_t other)
 }
 
 // This lane's part of a result row (columns 32 ct + place(e, h)) times `by`, to `row` in storage type; zeros where the row lies
-// behind its sequence.  Returns whether it holds an infinity or NaN.  (Columns from d on hold what the tile's
-// columns there held, which are the row's first ones again: no others that are odd.)
+// behind its sequence.
 template <int D>
-__device__ __forceinline__ bool store_row(const f32x16 (&acc)[D / 32], float by, bool there, bf16_t *row, int d, int h)
+__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], float by, bool there, bf16_t *row, int d, int h)
 {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    float probe = 0.f;
 #pragma unroll
     for (int ct = 0; ct < D / 32; ++ct)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             f32x4 v;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = there ? acc[ct][e + k] * by : 0.f;
-                probe = __builtin_fmaf(v[k], 0.f, probe);
-            }
+            for (int k = 0; k < 4; ++k) v[k] = there ? acc[ct][e + k] * by : 0.f;
             const int col = 32 * ct + 2 * e + 4 * h;
             if (col < d) *(bf16x4 *)(row + col) = __builtin_convertvector(v, bf16x4);
         }
+}
+
+// ---- walks without masked pairs ------------------------------------------------------------------
+// Where a result holds an infinity or NaN its wave walks its tiles again, straight from memory, 32 rows at a time: scores from
+// products as before, the sums pair by pair in fp32 over the pairs that see each other.  (In a tile's product a masked pair
+// counts as 0 times the other row, and 0 * inf would carry a token's infinity to rows that do not see it.)
+
+// acc += sum over the rows r of `rows` (32 of them) that this lane sees of w(r) times row r; w as results hold it
+template <int D>
+__device__ __forceinline__ void add_seen(const bf16_t *rows, int64_t ld, int d, const f32x16 &w, uint32_t seen, f32x16 (&acc)[D / 32])
+{
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5;
+#pragma unroll 1
+    for (int r = 0; r < 32; ++r) {
+        const int from = 4 * (r >> 3) + (r & 3);           // element of the result that holds row r, in half (r >> 2) & 1
+        float own = w[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) own = from == e ? w[e] : own;
+        const float by = __shfl(own, x + 32 * ((r >> 2) & 1));
+        if ((seen >> r) & 1u)
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int col = 32 * ct + 8 * e + 4 * h;
+                    if (col >= d) continue;
+                    const u2 v = *(const u2 *)(rows + r * ld + col);
+                    acc[ct][4 * e] += by * __uint_as_float(v.x << 16);
+                    acc[ct][4 * e + 1] += by * __uint_as_float(v.x & 0xffff0000u);
+                    acc[ct][4 * e + 2] += by * __uint_as_float(v.y << 16);
+                    acc[ct][4 * e + 3] += by * __uint_as_float(v.y & 0xffff0000u);
+                }
+    }
+}
+// scores of rows r0 .. r0 + 31 (row `last` for those behind it) with the wave's own row
+template <int D>
+__device__ __forceinline__ f32x16 far_scores(const bf16_t *rows, int64_t ld, int r0, int last, int d, const bf16x8 (&own)[D / 16])
+{
+    const int x = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
+    bf16x8 f[D / 16];
+    own_row<D>(rows + (int64_t)(r0 + x < last ? r0 + x : last) * ld, d, h, 1.f, f);
+    f32x16 c = {0};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) c = mfma32(f[s], own[s], c);
+    return c;
+}
+template <int CT>
+__device__ __forceinline__ bool odd_values(const f32x16 (&acc)[CT])
+{
+    float probe = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) probe = __builtin_fmaf(acc[ct][e], 0.f, probe);
     return probe != 0.f;
 }
 
-// Row i again, pair by pair in fp32 and without a masked pair: for rows whose result is not finite, so that an infinity
-// or NaN of a token that the row does not see leaves nothing in it (0 * inf in a tile's product).
 template <int D>
-__device__ __forceinline__ void fwd_row_again(const Window &w, const bf16_t *q, const bf16_t *K, const bf16_t *V, bf16_t *o, int i)
+__device__ __forceinline__ void fwd_again(const Window &w, const bf16_t *K, const bf16_t *V, const bf16x8 (&own)[D / 16], float c, int i0,
+                                          int i, int end, f32x16 (&acc)[D / 32], float &top, float &sum)
 {
-    const int lane = threadIdx.x & 63;
-    float top = -INFINITY, sum = 0.f, acc[D / 64];
+    const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int k = 0; k < D / 64; ++k) acc[k] = 0.f;
-    const KeyTiles tiles(w, i, i, 64);
+    for (int ct = 0; ct < D / 32; ++ct) acc[ct] = f32x16{0};
+    top = -INFINITY;
+    sum = 0.f;
+    const KeyTiles tiles(w, i0, i0 + kOwn < end ? i0 + kOwn - 1 : end - 1, 32);
     for (int k = 0; k < tiles.total; ++k) {
-        const int j = tiles.at(k) * 64 + lane;
-        const bool seen = window_sees(w, i, j);
-        float s = 0.f;
-        if (seen)
-            for (int c = 0; c < w.d; ++c) s += bf16_to_f32(q[c]) * bf16_to_f32(K[j * w.row_k + c]);
-        s = seen ? s * w.scale2 : -INFINITY;
-        float most = s;
+        const int j0 = tiles.at(k) * 32;
+        const uint32_t seen = i < end ? seen_keys(w, i, j0) : 0u;
+        f32x16 s = far_scores<D>(K, w.row_k, j0, end - 1, w.d, own);
+        branch_wait();
+        float most = -INFINITY;
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-        most = fmaxf(most, top);
-        const float less = top == -INFINITY ? 0.f : exp2f(top - most), p = seen ? exp2f(s - (most == -INFINITY ? 0.f : most)) : 0.f;
-        top = most;
-        float all = p;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) all += __shfl_xor(all, m);
-        sum = sum * less + all;
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) acc[c] *= less;
-        for (uint64_t bits = __ballot(seen); bits; bits &= bits - 1) {
-            const int from = __ffsll((long long)bits) - 1;
-            const float pj = __shfl(p, from);
-            const bf16_t *row = V + (tiles.at(k) * 64 + from) * w.row_k;
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c)
-                if (64 * c + lane < w.d) acc[c] += pj * bf16_to_f32(row[64 * c + lane]);
+        for (int e = 0; e < 16; ++e) {
+            s[e] = (seen >> place(e, h)) & 1u ? s[e] * c : -INFINITY;
+            most = fmaxf(most, s[e]);
         }
-    }
+        most = fmaxf(other_half(most, true), top);
+        const float less = top == -INFINITY ? 0.f : exp2f(top - most), base = most == -INFINITY ? 0.f : most;
+        top = most;
+        sum *= less;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-        if (64 * c + lane < w.d) o[64 * c + lane] = f32_to_bf16(acc[c] / sum);
+        for (int ct = 0; ct < D / 32; ++ct) acc[ct] *= less;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = exp2f(s[e] - base);
+            sum += s[e];
+        }
+        add_seen<D>(V + j0 * w.row_k, w.row_k, w.d, s, seen, acc);
+    }
 }
 
 template <int D>
@@ -242,7 +307,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
     __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES];
     const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
-    const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), unit = at_grid / groups;
+    const uint32_t at_grid = place_of<16>(blockIdx.x, gridDim.x), unit = at_grid / groups;
     const int first = (int)(groups - 1 - (at_grid - unit * groups)) * kOwnWg;      // long rows first
     const int b = unit / w.heads, head = unit - b * w.heads;
     const int end = window_end(lengths, b, w.n), i0 = first + kOwn * wave, i = i0 + x;
@@ -261,6 +326,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
         const KeyTiles tiles(w, first, last, kTile);
         const Tile stage(lds, d);
         const Reads<D> at(lane);
+        const uint32_t lds_at = lds_address(lds);
         stage.copy(k_rows, v_rows, w.row_k, tiles.at(0) * kTile, end, 0);
         for (int k = 0; k < tiles.total; ++k) {
             const int j0 = tiles.at(k) * kTile;
@@ -269,10 +335,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
             asm volatile("" ::: "memory");
             if (k + 1 < tiles.total) stage.copy(k_rows, v_rows, w.row_k, tiles.at(k + 1) * kTile, end, (k + 1) & 1);
             if (none_seen(w, i0, j0, kTile)) continue;
-            const unsigned char *tk = lds + (k & 1) * 2 * Tile::BYTES, *tv = tk + Tile::BYTES;
+            const uint32_t at_tile = lds_at + (k & 1) * 2 * Tile::BYTES;
+            const Reads<D> tk(at, at_tile), tv(at, at_tile + Tile::BYTES);
             f32x16 s[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) s[t] = scores<D>(at, tk, t, own);
+            for (int t = 0; t < 2; ++t) s[t] = scores<D>(tk, t, own);
+            read_ahead<2 * KS, 1, 4>();
             if (!all_seen(w, i0, j0, kTile)) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -302,105 +370,72 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
                     sum += s[t][e];
                 }
 #pragma unroll
-            for (int t = 0; t < 2; ++t) add_turned<D>(at, tv, t, s[t], acc);
+            for (int t = 0; t < 2; ++t) add_turned<D>(tv, t, s[t], acc);
             branch_wait();
+        }
+        if (__any(i < end && odd_values(acc))) {
+            own_row<D>(q + (i < end ? i : end - 1) * w.row_q, d, h, w.scale2, own);
+            fwd_again<D>(w, k_rows, v_rows, own, c, i0, i, end, acc, top, sum);
         }
     }
     sum = other_half(sum, false);
+    if (i >= w.n) return;
     const bool there = i < end;
-    bf16_t *o = O + b * w.batch_q + head * w.head_q;
-    bool odd = false;
-    if (i < w.n) {
-        odd = store_row<D>(acc, 1.f / sum, there, o + i * w.row_q, d, h);
-        if (lse && h == 0)
-            lse[((size_t)b * w.heads + head) * w.n + i] = there ? (top + __builtin_log2f(sum)) * kWindowLn2 : -INFINITY;
-    }
-    const uint64_t which = __ballot(odd);
-    for (uint32_t rows = (uint32_t)which | (uint32_t)(which >> 32); rows; rows &= rows - 1) {
-        const int r = i0 + __ffs((int)rows) - 1;
-        fwd_row_again<D>(w, q + r * w.row_q, k_rows, v_rows, o + r * w.row_q, r);
-    }
+    store_row<D>(acc, 1.f / sum, there, O + b * w.batch_q + head * w.head_q + i * w.row_q, d, h);
+    if (lse && h == 0)
+        lse[((size_t)b * w.heads + head) * w.n + i] = there ? (top + __builtin_log2f(sum)) * kWindowLn2 : -INFINITY;
 }
 
 // ---- backward ---------------------------------------------------------------------------------
 
-// Row i of dQ again (see fwd_row_again).
 template <int D>
-__device__ __forceinline__ void dq_row_again(const Window &w, const bf16_t *q, const bf16_t *g, const bf16_t *K, const bf16_t *V,
-                                             float L, float dot, bf16_t *dq, int i)
+__device__ __forceinline__ void dq_again(const Window &w, const bf16_t *K, const bf16_t *V, const bf16x8 (&own)[D / 16],
+                                         const bf16x8 (&own_g)[D / 16], float c, float L, float dot, int i0, int i, int end,
+                                         f32x16 (&acc)[D / 32])
 {
-    const int lane = threadIdx.x & 63;
-    float acc[D / 64];
+    const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int k = 0; k < D / 64; ++k) acc[k] = 0.f;
-    const KeyTiles tiles(w, i, i, 64);
+    for (int ct = 0; ct < D / 32; ++ct) acc[ct] = f32x16{0};
+    const KeyTiles tiles(w, i0, i0 + kOwn < end ? i0 + kOwn - 1 : end - 1, 32);
     for (int k = 0; k < tiles.total; ++k) {
-        const int j = tiles.at(k) * 64 + lane;
-        const bool seen = window_sees(w, i, j);
-        float s = 0.f, t = 0.f;
-        if (seen)
-            for (int c = 0; c < w.d; ++c) {
-                s += bf16_to_f32(q[c]) * bf16_to_f32(K[j * w.row_k + c]);
-                t += bf16_to_f32(g[c]) * bf16_to_f32(V[j * w.row_k + c]);
-            }
-        const float ds = exp2f(s * w.scale2 - L) * (t - dot);
-        for (uint64_t bits = __ballot(seen); bits; bits &= bits - 1) {
-            const int from = __ffsll((long long)bits) - 1;
-            const float by = __shfl(ds, from);
-            const bf16_t *row = K + (tiles.at(k) * 64 + from) * w.row_k;
+        const int j0 = tiles.at(k) * 32;
+        f32x16 s = far_scores<D>(K, w.row_k, j0, end - 1, w.d, own);
+        const f32x16 u = far_scores<D>(V, w.row_k, j0, end - 1, w.d, own_g);
+        branch_wait();
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c)
-                if (64 * c + lane < w.d) acc[c] += by * bf16_to_f32(row[64 * c + lane]);
-        }
+        for (int e = 0; e < 16; ++e) s[e] = exp2f(__builtin_fmaf(s[e], c, -L)) * (u[e] - dot);
+        add_seen<D>(K + j0 * w.row_k, w.row_k, w.d, s, i < end ? seen_keys(w, i, j0) : 0u, acc);
     }
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-        if (64 * c + lane < w.d) dq[64 * c + lane] = f32_to_bf16(acc[c] * w.scale);
 }
 
-// Row j of dK and dV again.  Q, dO, lse, delta: of the first query head of the key head in this batch.
+// Tiles [begin, stop) of a walk of the key side (see QueryTiles; tiles of `size` rows).
 template <int D>
-__device__ __forceinline__ void dkv_row_again(const Window &w, const bf16_t *k, const bf16_t *v, const bf16_t *Q, const bf16_t *dO,
-                                              const float *lse, const float *delta, int end, bf16_t *dk, bf16_t *dv, int j)
+__device__ __forceinline__ void dkv_again(const Window &w, const bf16_t *Q, const bf16_t *dO, const float *lse, const float *delta,
+                                          const bf16x8 (&own)[D / 16], const bf16x8 (&own_v)[D / 16], float c, int j, int end,
+                                          const QueryTiles &tiles, int size, int begin, int stop, f32x16 (&acc_k)[D / 32],
+                                          f32x16 (&acc_v)[D / 32])
 {
-    const int lane = threadIdx.x & 63;
-    float acc_k[D / 64], acc_v[D / 64];
+    const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) acc_k[c] = acc_v[c] = 0.f;
-    const int64_t reach = j < w.sinks ? (int64_t)end : (int64_t)j + w.window;
-    const int stop = reach < end ? (int)reach : end;
-    for (int head = 0; head < w.group; ++head)
-        for (int at = j; at < stop; at += 64) {
-            const int i = at + lane;
-            const bool seen = i < stop;
-            float s = 0.f, t = 0.f, p = 0.f, ds = 0.f;
-            if (seen) {
-                const int64_t row = head * w.head_q + i * w.row_q;
-                for (int c = 0; c < w.d; ++c) {
-                    s += bf16_to_f32(Q[row + c]) * bf16_to_f32(k[c]);
-                    t += bf16_to_f32(dO[row + c]) * bf16_to_f32(v[c]);
-                }
-                p = exp2f(s * w.scale2 - lse[(size_t)head * w.n + i] * kWindowLog2e);
-                ds = p * (t - delta[(size_t)head * w.n + i]);
+    for (int ct = 0; ct < D / 32; ++ct) acc_k[ct] = acc_v[ct] = f32x16{0};
+    for (int k = begin; k < stop; ++k) {
+        const int head = k / tiles.count, first = (tiles.tile0 + k - head * tiles.count) * size;
+        const bf16_t *q = Q + head * w.head_q, *g = dO + head * w.head_q;
+        for (int i0 = first; i0 < first + size && i0 < end; i0 += 32) {
+            f32x16 s = far_scores<D>(q, w.row_q, i0, end - 1, w.d, own);
+            f32x16 u = far_scores<D>(g, w.row_q, i0, end - 1, w.d, own_v);
+            branch_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = i0 + place(e, h) < end ? i0 + place(e, h) : end - 1;
+                s[e] = exp2f(__builtin_fmaf(s[e], c, -lse[(size_t)head * w.n + i] * kWindowLog2e));
+                u[e] = s[e] * (u[e] - delta[(size_t)head * w.n + i]);
             }
-            for (uint64_t bits = __ballot(seen); bits; bits &= bits - 1) {
-                const int from = __ffsll((long long)bits) - 1;
-                const float by_k = __shfl(ds, from), by_v = __shfl(p, from);
-                const int64_t row = head * w.head_q + (at + from) * w.row_q;
-#pragma unroll
-                for (int c = 0; c < D / 64; ++c)
-                    if (64 * c + lane < w.d) {
-                        acc_k[c] += by_k * bf16_to_f32(Q[row + 64 * c + lane]);
-                        acc_v[c] += by_v * bf16_to_f32(dO[row + 64 * c + lane]);
-                    }
-            }
+            const uint32_t seen = j < end ? seen_by(w, j, i0, end) : 0u;
+            add_seen<D>(g + i0 * w.row_q, w.row_q, w.d, s, seen, acc_v);
+            add_seen<D>(q + i0 * w.row_q, w.row_q, w.d, u, seen, acc_k);
         }
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-        if (64 * c + lane < w.d) {
-            dk[64 * c + lane] = f32_to_bf16(acc_k[c] * w.scale);
-            dv[64 * c + lane] = f32_to_bf16(acc_v[c]);
-        }
+    }
 }
 
 // dQ, and D = <dO, o> of every row for the kernel below.
@@ -415,7 +450,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
     __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES];
     const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
-    const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), unit = at_grid / groups;
+    const uint32_t at_grid = place_of<16>(blockIdx.x, gridDim.x), unit = at_grid / groups;
     const int first = (int)(groups - 1 - (at_grid - unit * groups)) * kOwnWg;
     const int b = unit / w.heads, head = unit - b * w.heads;
     const int end = window_end(lengths, b, w.n), i0 = first + kOwn * wave, i = i0 + x;
@@ -448,6 +483,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
         L = lse[row] * kWindowLog2e;
         if (i < end && h == 0) delta[row] = dot;
         const Reads<D> at(lane);
+        const uint32_t lds_at = lds_address(lds);
         for (int k = 0; k < tiles.total; ++k) {
             const int j0 = tiles.at(k) * kTile;
             wait_all_memory();
@@ -455,31 +491,31 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
             asm volatile("" ::: "memory");
             if (k + 1 < tiles.total) stage.copy(k_rows, v_rows, w.row_k, tiles.at(k + 1) * kTile, end, (k + 1) & 1);
             if (none_seen(w, i0, j0, kTile)) continue;
-            const unsigned char *tk = lds + (k & 1) * 2 * Tile::BYTES, *tv = tk + Tile::BYTES;
+            const uint32_t at_tile = lds_at + (k & 1) * 2 * Tile::BYTES;
+            const Reads<D> tk(at, at_tile), tv(at, at_tile + Tile::BYTES);
             const bool all = all_seen(w, i0, j0, kTile);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                f32x16 s = scores<D>(at, tk, t, own);
-                const f32x16 u = scores<D>(at, tv, t, own_g);
+                f32x16 s = scores<D>(tk, t, own);
+                const f32x16 u = scores<D>(tv, t, own_g);
+                read_ahead<2 * KS, 1, 4>();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -L)) * (u[e] - dot);
                 if (!all) {
                     const uint32_t bits = seen_keys(w, i, j0 + 32 * t) >> (4 * h);
                     static_for<16>([&](auto e) { s[int(e)] = pick<e>(bits, s[int(e)], 0u); });
                 }
-                add_turned<D>(at, tk, t, s, acc);
+                add_turned<D>(tk, t, s, acc);
             }
             branch_wait();
         }
+        if (__any(i < end && odd_values(acc))) {
+            own_row<D>(Q + at_q + safe * w.row_q, d, h, w.scale2, own);
+            own_row<D>(dO + at_q + safe * w.row_q, d, h, 1.f, own_g);
+            dq_again<D>(w, k_rows, v_rows, own, own_g, c, L, dot, i0, i, end, acc);
+        }
     }
-    bool odd = false;
-    if (i < w.n) odd = store_row<D>(acc, w.scale, i < end, dQ + at_q + i * w.row_q, d, h);
-    const uint64_t which = __ballot(odd);
-    for (uint32_t rows = (uint32_t)which | (uint32_t)(which >> 32); rows; rows &= rows - 1) {
-        const int at = __ffs((int)rows) - 1, r = i0 + at;
-        const int64_t row = at_q + r * w.row_q;
-        dq_row_again<D>(w, Q + row, dO + row, k_rows, v_rows, __shfl(L, at), __shfl(dot, at), dQ + row, r);
-    }
+    if (i < w.n) store_row<D>(acc, w.scale, i < end, dQ + at_q + i * w.row_q, d, h);
 }
 
 template <int D>
@@ -494,7 +530,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
     __shared__ float2 row_data[2][TILE];                  // L (in exponents of 2) and D of the tile's rows
     const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
-    const uint32_t at_grid = place_of(blockIdx.x, gridDim.x), each = walks.each(), unit = at_grid / each;
+    const uint32_t at_grid = place_of<2>(blockIdx.x, gridDim.x), each = walks.each(), unit = at_grid / each;
     const KeyWalk walk(walks, at_grid - unit * each);
     const int group = walk.group, part = walk.part, parts = walk.parts;
     const int first = group * kOwnWg;
@@ -528,14 +564,16 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
         int now = tile;
         if (begin < stop) copy(0);
         const Reads<D> at(lane);
+        const uint32_t lds_at = lds_address(lds);
         bf16x8 own[KS], own_v[V_IN_LDS ? 1 : KS];
         own_row<D>(K + at_k + (j < end ? j : end - 1) * w.row_k, d, h, w.scale2, own);
-        unsigned char *wave_v = lds + 2 * 2 * Tile::BYTES + wave * (kOwn * D * 2);
+        const Reads<D> mine(at, lds_at + 2 * 2 * Tile::BYTES + wave * (kOwn * D * 2));   // the wave's value rows
         if constexpr (V_IN_LDS) {
             bf16x8 v[KS];
             own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, v);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) *(bf16x8 *)(wave_v + at.along[s]) = v[s];   // (read by this wave alone)
+            for (int s = 0; s < KS; ++s)                      // (read by this wave alone)
+                *(__attribute__((address_space(3))) bf16x8 *)(uintptr_t)(mine.along ^ (32 * s)) = v[s];
         } else own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, own_v);
         for (int k = begin; k < stop; ++k) {
             const int buf = (k - begin) & 1, i0 = (tiles.tile0 + now) * TILE;
@@ -548,16 +586,22 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
             const bool none = i0 + TILE - 1 < j0 || (i0 - (j0 + kOwn - 1) >= w.window && j0 >= w.sinks);
             if (none) continue;
             const bool all = i0 >= j0 + kOwn - 1 && (i0 + TILE - 1 - j0 < w.window || j0 + kOwn <= w.sinks) && i0 + TILE <= end;
-            const unsigned char *tq = lds + buf * 2 * Tile::BYTES, *tg = tq + Tile::BYTES;
+            const uint32_t at_tile = lds_at + buf * 2 * Tile::BYTES;
+            const Reads<D> tq(at, at_tile), tg(at, at_tile + Tile::BYTES);
 #pragma unroll
             for (int t = 0; t < TILE / 32; ++t) {
-                f32x16 s = scores<D>(at, tq, t, own);
+                f32x16 s = scores<D>(tq, t, own);
                 f32x16 u = {0};
 #pragma unroll
                 for (int q = 0; q < KS; ++q) {
-                    if constexpr (V_IN_LDS) u = mfma32(at.row(tg, t, q), at.row(wave_v, 0, q), u);
-                    else u = mfma32(at.row(tg, t, q), own_v[q], u);
+                    if constexpr (V_IN_LDS) u = mfma32(tg.row(t, q), mine.row(0, q), u);
+                    else u = mfma32(tg.row(t, q), own_v[q], u);
                 }
+                if constexpr (V_IN_LDS) {
+                    read_ahead<KS, 1, 4>();
+                    read_ahead<KS, 2, 2>();
+                    __builtin_amdgcn_sched_barrier(0);     // (else the reads of row_data get into the order above)
+                } else read_ahead<2 * KS, 1, 4>();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float2 r = row_data[buf][32 * t + place(e, h)];
@@ -571,10 +615,16 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
                         u[int(e)] = pick<e>(bits, u[int(e)], 0u);
                     });
                 }
-                add_turned<D>(at, tg, t, s, acc_v);
-                add_turned<D>(at, tq, t, u, acc_k);
+                add_turned<D>(tg, t, s, acc_v);
+                add_turned<D>(tq, t, u, acc_k);
             }
             branch_wait();
+        }
+        if (__any(j < end && (odd_values(acc_k) || odd_values(acc_v)))) {
+            bf16x8 v[KS];
+            own_row<D>(K + at_k + (j < end ? j : end - 1) * w.row_k, d, h, w.scale2, own);
+            own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, v);
+            dkv_again<D>(w, Q + at_q, dO + at_q, lse + at_rows, delta + at_rows, own, v, c, j, end, tiles, TILE, begin, stop, acc_k, acc_v);
         }
     }
     if (parts > 1) {                                       // a share: [unit][group][part][dK, dV][128][d], added below
@@ -593,55 +643,30 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
             }
         return;
     }
-    bool odd = false;
-    if (j < w.n) {
-        odd = store_row<D>(acc_k, w.scale, j < end, dK + at_k + j * w.row_k, d, h);
-        odd |= store_row<D>(acc_v, 1.f, j < end, dV + at_k + j * w.row_k, d, h);
-    }
-    const uint64_t bad = __ballot(odd);
-    for (uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32); rows; rows &= rows - 1) {
-        const int r = j0 + __ffs((int)rows) - 1;
-        const int64_t row = at_k + r * w.row_k;
-        dkv_row_again<D>(w, K + row, V + row, Q + at_q, dO + at_q, lse + at_rows, delta + at_rows, end, dK + row, dV + row, r);
-    }
+    if (j >= w.n) return;
+    store_row<D>(acc_k, w.scale, j < end, dK + at_k + j * w.row_k, d, h);
+    store_row<D>(acc_v, 1.f, j < end, dV + at_k + j * w.row_k, d, h);
 }
 
-// The shares of the first tokens' gradients added in order: a wave a row of 128, lanes are columns.
-template <int D>
-__global__ __launch_bounds__(kThreads) void window_share_kernel(const bf16_t *Q, const bf16_t *K, const bf16_t *V,
-                                                                const int32_t *lengths, const float *lse, const bf16_t *dO,
-                                                                const float *delta, bf16_t *dK, bf16_t *dV, const float *room,
-                                                                Window w, KeyWalks walks)
+// The shares of the first tokens' gradients added in order: a thread four columns of a row.
+__global__ __launch_bounds__(kThreads) void window_share_kernel(bf16_t *dK, bf16_t *dV, const float *room, Window w, KeyWalks walks)
 {
-    const int lane = threadIdx.x & 63, d = w.d;
-    const uint32_t row = blockIdx.x * kWaves + (threadIdx.x >> 6), block = row / kOwnWg;
-    const int in_block = row % kOwnWg, unit = block / walks.few, group = block - unit * walks.few, j = group * kOwnWg + in_block;
-    const int b = unit / w.kv_heads, kv = unit - b * w.kv_heads;
-    if (j >= w.n) return;
-    const int end = window_end(lengths, b, w.n);
-    const int64_t at_k = b * w.batch_k + kv * w.head_k, at_q = b * w.batch_q + (int64_t)kv * w.group * w.head_q, to = at_k + j * w.row_k;
-    const size_t at_rows = ((size_t)b * w.heads + kv * w.group) * w.n;
-    const float *from = room + (size_t)block * walks.parts * 2 * kOwnWg * d + (size_t)in_block * d;
-    bool odd = false;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-        const int col = 64 * c + lane;
-        float k = 0.f, v = 0.f;
-        if (col < d && j < end) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const int pieces = w.d / 4, at = blockIdx.x * kThreads + threadIdx.x, row = at / pieces, c = 4 * (at - row * pieces);
+    const int b = blockIdx.y / w.kv_heads, kv = blockIdx.y - b * w.kv_heads;
+    if (row >= walks.few * kOwnWg || row >= w.n) return;
+    const size_t share = 2 * (size_t)kOwnWg * w.d;
+    const float *from = room + ((size_t)blockIdx.y * walks.few + row / kOwnWg) * walks.parts * share + (size_t)(row % kOwnWg) * w.d + c;
+    f32x4 k = {0.f, 0.f, 0.f, 0.f}, v = k;
 #pragma unroll 4
-            for (int p = 0; p < walks.parts; ++p) {
-                k += from[(size_t)p * 2 * kOwnWg * d + col];
-                v += from[(size_t)p * 2 * kOwnWg * d + (size_t)kOwnWg * d + col];
-            }
-            k *= w.scale;
-            odd |= !(fabsf(k) < INFINITY) || !(fabsf(v) < INFINITY);
-        }
-        if (col < d) {
-            dK[to + col] = f32_to_bf16(k);
-            dV[to + col] = f32_to_bf16(v);
-        }
+    for (int p = 0; p < walks.parts; ++p) {
+        k += *(const f32x4 *)(from + p * share);
+        v += *(const f32x4 *)(from + p * share + share / 2);
     }
-    if (__any(odd)) dkv_row_again<D>(w, K + to, V + to, Q + at_q, dO + at_q, lse + at_rows, delta + at_rows, end, dK + to, dV + to, j);
+    const int64_t to = b * w.batch_k + kv * w.head_k + row * w.row_k + c;
+    *(bf16x4 *)(dK + to) = __builtin_convertvector(k * w.scale, bf16x4);
+    *(bf16x4 *)(dV + to) = __builtin_convertvector(v, bf16x4);
 }
 
 KeyWalks walks_of(const Window &w) { return key_walks(w, kOwnWg, w.d <= 64 ? 64 : 32); }
@@ -683,8 +708,8 @@ psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
                            p.delta, dK, dV, p.room, w, walks);
         PSF_LAUNCH_CHECK();
         if (walks.parts == 1) return PSF_OK;
-        hipLaunchKernelGGL((window_share_kernel<D>), dim3(units * walks.few * kOwnWg / kWaves), dim3(kThreads), 0, s, Q, K, V,
-                           p.lengths, p.lse, dO, p.delta, dK, dV, p.room, w, walks);
+        hipLaunchKernelGGL(window_share_kernel, dim3((walks.few * kOwnWg * (w.d / 4) + kThreads - 1) / kThreads, units), dim3(kThreads), 0,
+                           s, dK, dV, p.room, w, walks);
         PSF_LAUNCH_CHECK();
         return PSF_OK;
     };
