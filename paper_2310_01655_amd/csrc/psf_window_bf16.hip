@@ -186,23 +186,34 @@ __device__ __forceinline__ float pick(uint32_t bits_h, float x, uint32_t other)
     return __uint_as_float((__float_as_uint(x) & mask) | (other & ~mask));
 }
 
-// This lane's part of a result row (columns 32 ct + place(e, h)) times `by`, to `row` in storage type; zeros where the row lies
-// behind its sequence.
+// The wave's 32 result rows times `by` to memory in storage type (rows that lie behind their sequence: zeros): through LDS,
+// where every lane has 8-byte pieces of its own row (columns 32 ct + place(e, h)) and takes whole 16-byte pieces of 64 / (D / 8)
+// rows at a time, so that lines are written whole.  at: LDS address of the wave's 64 D bytes; to: its first row;
+// rows: how many of them exist.
 template <int D>
-__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], float by, bool there, bf16_t *row, int d, int h)
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float by, bool there, uint32_t at, bf16_t *to, int64_t ld, int rows,
+                                           int d, int lane)
 {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    const int x = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int ct = 0; ct < D / 32; ++ct)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
+        for (int e = 0; e < 4; ++e) {
             f32x4 v;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = there ? acc[ct][e + k] * by : 0.f;
-            const int col = 32 * ct + 2 * e + 4 * h;
-            if (col < d) *(bf16x4 *)(row + col) = __builtin_convertvector(v, bf16x4);
+            for (int k = 0; k < 4; ++k) v[k] = there ? acc[ct][4 * e + k] * by : 0.f;
+            *(__attribute__((address_space(3))) bf16x4 *)(uintptr_t)(at + x * (D * 2) + ((4 * ct + e) ^ row_swz<D>(x)) * 16 + 8 * h) =
+                __builtin_convertvector(v, bf16x4);
         }
+#pragma unroll
+    for (int q = 0; q < D / 16; ++q) {
+        const int slot = q * 64 + lane, row = slot / (D / 8), piece = slot % (D / 8);
+        const u4 v = *(__attribute__((address_space(3))) const u4 *)(uintptr_t)(at + row * (D * 2) + (piece ^ row_swz<D>(row)) * 16);
+        if (row < rows && 8 * piece < d) *(u4 *)(to + row * ld + 8 * piece) = v;
+    }
 }
 
 // ---- walks without masked pairs ------------------------------------------------------------------
@@ -379,10 +390,11 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
         }
     }
     sum = other_half(sum, false);
-    if (i >= w.n) return;
     const bool there = i < end;
-    store_row<D>(acc, 1.f / sum, there, O + b * w.batch_q + head * w.head_q + i * w.row_q, d, h);
-    if (lse && h == 0)
+    __syncthreads();                                       // (the tiles have been read)
+    store_rows<D>(acc, 1.f / sum, there, lds_address(lds) + wave * (64 * D), O + b * w.batch_q + head * w.head_q + i0 * w.row_q, w.row_q,
+                  w.n - i0, d, lane);
+    if (lse && h == 0 && i < w.n)
         lse[((size_t)b * w.heads + head) * w.n + i] = there ? (top + __builtin_log2f(sum)) * kWindowLn2 : -INFINITY;
 }
 
@@ -515,7 +527,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
             dq_again<D>(w, k_rows, v_rows, own, own_g, c, L, dot, i0, i, end, acc);
         }
     }
-    if (i < w.n) store_row<D>(acc, w.scale, i < end, dQ + at_q + i * w.row_q, d, h);
+    __syncthreads();
+    store_rows<D>(acc, w.scale, i < end, lds_address(lds) + wave * (64 * D), dQ + at_q + i0 * w.row_q, w.row_q, w.n - i0, d, lane);
 }
 
 template <int D>
@@ -643,9 +656,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
             }
         return;
     }
-    if (j >= w.n) return;
-    store_row<D>(acc_k, w.scale, j < end, dK + at_k + j * w.row_k, d, h);
-    store_row<D>(acc_v, 1.f, j < end, dV + at_k + j * w.row_k, d, h);
+    __syncthreads();
+    const uint32_t rows_at = lds_address(lds) + wave * (64 * D);
+    store_rows<D>(acc_k, w.scale, j < end, rows_at, dK + at_k + j0 * w.row_k, w.row_k, w.n - j0, d, lane);
+    store_rows<D>(acc_v, 1.f, j < end, rows_at, dV + at_k + j0 * w.row_k, w.row_k, w.n - j0, d, lane);
 }
 
 // The shares of the first tokens' gradients added in order: a thread four columns of a row.
