@@ -307,9 +307,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const T *x, cons
                 for (int e = 0; e < N; ++e) fold[threadIdx.x * (N + 1) + e] = v[e];
                 __syncthreads();
                 if (threadIdx.x < G)
+#pragma unroll 1
+                    for (int r = 1; r < ROWS; ++r)
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        for (int r = 1; r < ROWS; ++r) v[e] += fold[(threadIdx.x + r * G) * (N + 1) + e];
+                        for (int e = 0; e < N; ++e) v[e] += fold[(threadIdx.x + r * G) * (N + 1) + e];
             }
             if (threadIdx.x < G)
 #pragma unroll
@@ -357,7 +358,8 @@ psf_status norm_shape(int width, F &&go)
     if (pieces <= 256) return with(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
     if (pieces <= 512) return with(std::integral_constant<int, kNormWide>{}, std::integral_constant<int, 2>{});
     if (pieces <= 1024) return with(std::integral_constant<int, kNormWide>{}, std::integral_constant<int, 4>{});
-    return with(std::integral_constant<int, kNormWide>{}, std::integral_constant<int, 8>{});
+    if constexpr (PSF_NORM_MAX_WIDTH / Piece<T>::N > 1024) return with(std::integral_constant<int, kNormWide>{}, std::integral_constant<int, 8>{});
+    return PSF_ERR_UNSUPPORTED;                             // (not reached: check())
 }
 
 // Rows in flight for every group of lanes: enough bytes a lane to cover the memory's latency.

@@ -43,6 +43,28 @@ __device__ __forceinline__ bool window_sees(const Window &w, int i, int j)
     return j <= i && (i - j < w.window || j < w.sinks);
 }
 
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+// keys j0 .. j0 + 31 that row i sees, as bits
+__device__ __forceinline__ uint32_t seen_keys(const Window &w, int i, int j0)
+{
+    return bits_below(i - j0 + 1) & (~bits_below(i - w.window + 1 - j0) | bits_below(w.sinks - j0));
+}
+// rows i0 .. i0 + 31 below `end` that see key j, as bits
+__device__ __forceinline__ uint32_t seen_by(const Window &w, int j, int i0, int end)
+{
+    const int64_t reach = j < w.sinks ? (int64_t)end : (int64_t)j + w.window;
+    return bits_below((reach < end ? (int)reach : end) - i0) & ~bits_below(j - i0);
+}
+// Whether rows [i0, i0 + rows - 1] see all / none of keys [j0, j0 + len - 1].
+__device__ __forceinline__ bool all_seen(const Window &w, int i0, int rows, int j0, int len)
+{
+    return j0 + len - 1 <= i0 && (i0 + rows - 1 - j0 < w.window || j0 + len <= w.sinks);
+}
+__device__ __forceinline__ bool none_seen(const Window &w, int i0, int rows, int j0, int len)
+{
+    return j0 > i0 + rows - 1 || (i0 - (j0 + len - 1) >= w.window && j0 >= w.sinks);
+}
+
 // The tiles of `size` keys that rows [first, last] see some of: those of the first tokens, then those of the window.
 struct KeyTiles {
     int few, window_first, total;

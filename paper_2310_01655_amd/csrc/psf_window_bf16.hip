@@ -140,16 +140,6 @@ __device__ __forceinline__ void add_turned(const Reads<D> &tile, int t, const f3
 // place in its 32 rows of element e of a result
 __device__ __forceinline__ int place(int e, int h) { return 8 * (e / 4) + 4 * h + e % 4; }
 
-// Whether rows [i0, i0 + 31] see all / none of keys [j0, j0 + len - 1].
-__device__ __forceinline__ bool all_seen(const Window &w, int i0, int j0, int len)
-{
-    return j0 + len - 1 <= i0 && (i0 + kOwn - 1 - j0 < w.window || j0 + len <= w.sinks);
-}
-__device__ __forceinline__ bool none_seen(const Window &w, int i0, int j0, int len)
-{
-    return j0 > i0 + kOwn - 1 || (i0 - (j0 + len - 1) >= w.window && j0 >= w.sinks);
-}
-
 // Which workgroup of the call (unit by unit, neighbouring rows side by side) workgroup `id` of the launch is.  The launch
 // deals its workgroups out to the 8 XCDs in turn; runs of RUN neighbours stay on one XCD, whose L2 serves the
 // tiles that they share, and the runs go round the XCDs, one further every time round, so that neither sequences
@@ -164,18 +154,6 @@ __device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t total)
     return (round * 8 + (id + round) % 8) * RUN + slot % RUN;
 }
 
-__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
-// keys j0 .. j0 + 31 that row i sees, as bits
-__device__ __forceinline__ uint32_t seen_keys(const Window &w, int i, int j0)
-{
-    return bits_below(i - j0 + 1) & (~bits_below(i - w.window + 1 - j0) | bits_below(w.sinks - j0));
-}
-// rows i0 .. i0 + 31 below `end` that see key j, as bits
-__device__ __forceinline__ uint32_t seen_by(const Window &w, int j, int i0, int end)
-{
-    const int64_t reach = j < w.sinks ? (int64_t)end : (int64_t)j + w.window;
-    return bits_below((reach < end ? (int)reach : end) - i0) & ~bits_below(j - i0);
-}
 // x where bit place(E, h) of the row's bits is set, `other` elsewhere; bits_h: those bits >> 4 h.  (The bit as a mask, by an
 // instruction of its own: as a comparison and a select it takes five.)
 template <int E>
@@ -345,14 +323,14 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(const bf16_t *Q
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (k + 1 < tiles.total) stage.copy(k_rows, v_rows, w.row_k, tiles.at(k + 1) * kTile, end, (k + 1) & 1);
-            if (none_seen(w, i0, j0, kTile)) continue;
+            if (none_seen(w, i0, kOwn, j0, kTile)) continue;
             const uint32_t at_tile = lds_at + (k & 1) * 2 * Tile::BYTES;
             const Reads<D> tk(at, at_tile), tv(at, at_tile + Tile::BYTES);
             f32x16 s[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) s[t] = scores<D>(tk, t, own);
             read_ahead<2 * KS, 1, 4>();
-            if (!all_seen(w, i0, j0, kTile)) {
+            if (!all_seen(w, i0, kOwn, j0, kTile)) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const uint32_t bits = seen_keys(w, i, j0 + 32 * t) >> (4 * h);
@@ -502,10 +480,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (k + 1 < tiles.total) stage.copy(k_rows, v_rows, w.row_k, tiles.at(k + 1) * kTile, end, (k + 1) & 1);
-            if (none_seen(w, i0, j0, kTile)) continue;
+            if (none_seen(w, i0, kOwn, j0, kTile)) continue;
             const uint32_t at_tile = lds_at + (k & 1) * 2 * Tile::BYTES;
             const Reads<D> tk(at, at_tile), tv(at, at_tile + Tile::BYTES);
-            const bool all = all_seen(w, i0, j0, kTile);
+            const bool all = all_seen(w, i0, kOwn, j0, kTile);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 f32x16 s = scores<D>(tk, t, own);
@@ -531,15 +509,17 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
     store_rows<D>(acc, w.scale, i < end, lds_address(lds) + wave * (64 * D), dQ + at_q + i0 * w.row_q, w.row_q, w.n - i0, d, lane);
 }
 
+// dK and dV.  The wave's values lie in LDS: with them in registers three waves a SIMD do not fit at d = 64 (161 us instead of 145,
+// see place_of) and two do not at d = 128 (1850 us instead of 1100, 2 x 16 x 16384, window 4096, one sequence empty), where the
+// tiles are of 32 queries, so that two workgroups share a CU.
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void window_dkv_kernel(
     const bf16_t *Q, const bf16_t *K, const bf16_t *V, const int32_t *lengths, const float *lse, const bf16_t *dO,
     const float *delta, bf16_t *dK, bf16_t *dV, float *room, Window w, KeyWalks walks)
 {
     constexpr int KS = D / 16, CT = D / 32, TILE = D == 64 ? 64 : 32;
-    constexpr bool V_IN_LDS = D == 128;
     using Tile = Staged<D, TILE>;
-    __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES + (V_IN_LDS ? kOwnWg * D * 2 : 0)];
+    __shared__ __align__(1024) unsigned char lds[2 * 2 * Tile::BYTES + kOwnWg * D * 2];
     __shared__ float2 row_data[2][TILE];                  // L (in exponents of 2) and D of the tile's rows
     const int lane = threadIdx.x & 63, x = lane & 31, h = lane >> 5, d = w.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (in a scalar register: which tiles count is the wave's)
@@ -578,16 +558,16 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
         if (begin < stop) copy(0);
         const Reads<D> at(lane);
         const uint32_t lds_at = lds_address(lds);
-        bf16x8 own[KS], own_v[V_IN_LDS ? 1 : KS];
+        bf16x8 own[KS];
         own_row<D>(K + at_k + (j < end ? j : end - 1) * w.row_k, d, h, w.scale2, own);
         const Reads<D> mine(at, lds_at + 2 * 2 * Tile::BYTES + wave * (kOwn * D * 2));   // the wave's value rows
-        if constexpr (V_IN_LDS) {
+        {
             bf16x8 v[KS];
             own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, v);
 #pragma unroll
-            for (int s = 0; s < KS; ++s)                      // (read by this wave alone)
+            for (int s = 0; s < KS; ++s)                   // (read by this wave alone)
                 *(__attribute__((address_space(3))) bf16x8 *)(uintptr_t)(mine.along ^ (32 * s)) = v[s];
-        } else own_row<D>(V + at_k + (j < end ? j : end - 1) * w.row_k, d, h, 1.f, own_v);
+        }
         for (int k = begin; k < stop; ++k) {
             const int buf = (k - begin) & 1, i0 = (tiles.tile0 + now) * TILE;
             now = tile;
@@ -606,15 +586,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(
                 f32x16 s = scores<D>(tq, t, own);
                 f32x16 u = {0};
 #pragma unroll
-                for (int q = 0; q < KS; ++q) {
-                    if constexpr (V_IN_LDS) u = mfma32(tg.row(t, q), mine.row(0, q), u);
-                    else u = mfma32(tg.row(t, q), own_v[q], u);
-                }
-                if constexpr (V_IN_LDS) {
-                    read_ahead<KS, 1, 4>();
-                    read_ahead<KS, 2, 2>();
-                    __builtin_amdgcn_sched_barrier(0);     // (else the reads of row_data get into the order above)
-                } else read_ahead<2 * KS, 1, 4>();
+                for (int q = 0; q < KS; ++q) u = mfma32(tg.row(t, q), mine.row(0, q), u);
+                read_ahead<KS, 1, 4>();
+                read_ahead<KS, 2, 2>();
+                __builtin_amdgcn_sched_barrier(0);         // (else the reads of row_data get into the order above)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float2 r = row_data[buf][32 * t + place(e, h)];

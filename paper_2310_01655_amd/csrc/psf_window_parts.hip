@@ -53,21 +53,8 @@ __device__ __forceinline__ void add_tile(const uint16_t *tile, int plane, int pi
     }
 }
 
-// bits of the tile's rows that row `i` (as a query) sees, keys from j0 on
-__device__ __forceinline__ unsigned seen_keys(const Window &w, int i, int j0, int end)
-{
-    unsigned m = 0;
-    if (i < end)
-        for (int k = 0; k < kTile; ++k) m |= window_sees(w, i, j0 + k) ? 1u << k : 0u;
-    return m;
-}
-// bits of the tile's rows (as queries from i0 on) that see key j
-__device__ __forceinline__ unsigned seen_by(const Window &w, int j, int i0, int end)
-{
-    unsigned m = 0;
-    for (int k = 0; k < kTile; ++k) m |= i0 + k < end && window_sees(w, i0 + k, j) ? 1u << k : 0u;
-    return m;
-}
+// This lane's eight places of a tile (tile order), as bits of it
+__device__ __forceinline__ constexpr int place(int e) { return 16 * (e / 4) + e % 4; }
 
 template <int NT, typename S>
 __global__ __launch_bounds__(256) void window_parts_fwd_kernel(const S *Q, const S *K, const S *V, const int32_t *lengths, S *O,
@@ -78,9 +65,10 @@ __global__ __launch_bounds__(256) void window_parts_fwd_kernel(const S *Q, const
     __shared__ uint16_t tk[P * Tiles::PLANE], tv[P * Tiles::PLANE];
     __shared__ int odd_seen;
     if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.y / w.heads, h = blockIdx.y % w.heads, d = w.d;
-    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, i = first + 16 * wave + li;
+    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, i0 = first + 16 * wave, i = i0 + li;
     const int64_t at_q = b * w.batch_q + h * w.head_q, at_k = b * w.batch_k + h / w.group * w.head_k;
     f4 acc[NT];
     clear(acc);
@@ -109,23 +97,28 @@ __global__ __launch_bounds__(256) void window_parts_fwd_kernel(const S *Q, const
             score_parts<2, KS, P, P>(tk, Tiles::PLANE, Tiles::PITCH, 0, own, lane, s);
             float w8[8], most = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = j0 + 16 * (e / 4) + 4 * g + e % 4;
-                w8[e] = i < end && window_sees(w, i, j) ? s[e / 4][e % 4] * w.scale2 : -INFINITY;
-                most = fmaxf(most, w8[e]);
+            for (int e = 0; e < 8; ++e) w8[e] = s[e / 4][e % 4] * w.scale2;
+            uint32_t seen = 0xffffffffu;                   // the tile's rows, as this row sees them
+            if (!all_seen(w, i0, 16, j0, kTile) || i0 + 15 >= end) {
+                seen = i < end ? seen_keys(w, i, j0) : 0u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(seen >> 4 * g >> place(e) & 1u)) w8[e] = -INFINITY;
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, w8[e]);
             most = fmaxf(top, max_over_groups(most));
-            const float less = top == -INFINITY ? 0.f : exp2f(top - most), base = most == -INFINITY ? 0.f : most;
+            const float less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most), base = most == -INFINITY ? 0.f : most;
             top = most;
             sum *= less;
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[t] *= less;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                w8[e] = exp2f(w8[e] - base);
+                w8[e] = __builtin_amdgcn_exp2f(w8[e] - base);
                 sum += w8[e];
             }
-            add_tile<NT, P>(tv, Tiles::PLANE, Tiles::PITCH, w8, acc, lane, odd & 2, odd & 2 ? seen_keys(w, i, j0, end) : 0u);
+            add_tile<NT, P>(tv, Tiles::PLANE, Tiles::PITCH, w8, acc, lane, odd & 2, seen);
         }
     }
     sum = over_groups(sum);
@@ -147,9 +140,10 @@ __global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const 
     __shared__ uint16_t tk[P * Tiles::PLANE], tv[P * Tiles::PLANE];
     __shared__ int odd_seen;
     if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.y / w.heads, h = blockIdx.y % w.heads, d = w.d;
-    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, i = first + 16 * wave + li;
+    const int end = window_end(lengths, b, w.n), first = blockIdx.x * kRows, i0 = first + 16 * wave, i = i0 + li;
     const int64_t at_q = b * w.batch_q + h * w.head_q, at_k = b * w.batch_k + h / w.group * w.head_k;
     f4 acc[NT];
     clear(acc);
@@ -193,12 +187,16 @@ __global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const 
             score_parts<2, KS, P, P>(tv, Tiles::PLANE, Tiles::PITCH, 0, own_g, lane, t);
             float w8[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = j0 + 16 * (e / 4) + 4 * g + e % 4;
-                const float p = exp2f(s[e / 4][e % 4] * w.scale2 - L);
-                w8[e] = i < end && window_sees(w, i, j) ? p * (t[e / 4][e % 4] - D) : 0.f;
+            for (int e = 0; e < 8; ++e)
+                w8[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 4][e % 4], w.scale2, -L)) * (t[e / 4][e % 4] - D);
+            uint32_t seen = 0xffffffffu;
+            if (!all_seen(w, i0, 16, j0, kTile) || i0 + 15 >= end) {
+                seen = i < end ? seen_keys(w, i, j0) : 0u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(seen >> 4 * g >> place(e) & 1u)) w8[e] = 0.f;
             }
-            add_tile<NT, P>(tk, Tiles::PLANE, Tiles::PITCH, w8, acc, lane, odd & 1, odd & 1 ? seen_keys(w, i, j0, end) : 0u);
+            add_tile<NT, P>(tk, Tiles::PLANE, Tiles::PITCH, w8, acc, lane, odd & 1, seen);
         }
     }
     if (i >= w.n) return;
@@ -218,10 +216,11 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
     __shared__ float rows_l[kTile], rows_d[kTile];
     __shared__ int odd_seen;
     if (threadIdx.x == 0) odd_seen = 0;                    // (the loop's first barrier comes before its first use)
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KeyWalk walk(walks, blockIdx.x);
     const int b = blockIdx.y / w.kv_heads, kv = blockIdx.y % w.kv_heads, d = w.d;
-    const int end = window_end(lengths, b, w.n), first = walk.group * kRows, own_at = 16 * wave + li, j = first + own_at;
+    const int end = window_end(lengths, b, w.n), first = walk.group * kRows, own_at = 16 * wave + li, j0 = first + 16 * wave, j = j0 + li;
     const int64_t at_k = b * w.batch_k + kv * w.head_k;
     f4 acc_k[NT], acc_v[NT];
     clear(acc_k);
@@ -267,12 +266,17 @@ __global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const
             float p8[8], w8[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int r = 16 * (e / 4) + 4 * g + e % 4, i = i0 + r;
-                const bool seen = i < end && j < end && window_sees(w, i, j);
-                p8[e] = seen ? exp2f(s[e / 4][e % 4] * w.scale2 - rows_l[r]) : 0.f;
-                w8[e] = seen ? p8[e] * (t[e / 4][e % 4] - rows_d[r]) : 0.f;
+                const int r = place(e) + 4 * g;
+                p8[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 4][e % 4], w.scale2, -rows_l[r]));
+                w8[e] = p8[e] * (t[e / 4][e % 4] - rows_d[r]);
             }
-            const unsigned seen = odd && j < end ? seen_by(w, j, i0, end) : 0u;
+            uint32_t seen = 0xffffffffu;                   // the tile's rows that see this key
+            if (i0 < j0 + 15 || (i0 + kTile - 1 - j0 >= w.window && j0 + 16 > w.sinks) || i0 + kTile > end || j0 + 15 >= end) {
+                seen = j < end ? seen_by(w, j, i0, end) : 0u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(seen >> 4 * g >> place(e) & 1u)) p8[e] = w8[e] = 0.f;
+            }
             add_tile<NT, P>(tg, Tiles::PLANE, Tiles::PITCH, p8, acc_v, lane, odd & 2, seen);
             add_tile<NT, P>(tq, Tiles::PLANE, Tiles::PITCH, w8, acc_k, lane, odd & 1, seen);
         }
