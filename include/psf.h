@@ -5,7 +5,8 @@
  * psf_causal_attn_bwd, psf_causal_attn_fwd_save + psf_causal_attn_bwd_saved (forward and
  * backward without a second forward pass), psf_decode_step (token by token) with
  * psf_decode_prefill (its state after a prompt), the *_timed variants for benchmarking, and the
- * host-only sizing / selection queries.
+ * host-only sizing / selection queries.  Around them: psf_layer_norm_*, softmax attention with a sliding
+ * window (psf_window_attn_*) and its single-token form over a paged cache (psf_paged_attn, psf_cache_*).
  *
  * Method: PolySketchFormer (arXiv 2310.01655).  Every query/key row x is mapped to
  *   m(x)    = PolySketchWithNegativity(x, r, p/2)            (Algorithm 1)
@@ -22,8 +23,9 @@
  *     frees or synchronises; all work is enqueued on `hip_stream` (a hipStream_t, NULL = the
  *     default stream).  Calls are re-entrant as long as workspaces do not overlap.
  *   - Tensors are dense row-major: Q, K, M [batch, heads, n, d|r]; V, O [batch, heads, n, dv].
- *   - The library neither normalises Q/K (the paper applies layer normalisation before the
- *     kernel, Section 2.1) nor applies a 1/sqrt(d) scale (the final definition has none).
+ *   - The attention calls neither normalise Q/K (the paper applies layer normalisation before the
+ *     kernel, Section 2.1: psf_layer_norm_fwd) nor, but for psf_window_attn_* and psf_paged_attn, apply a
+ *     1/sqrt(d) scale (the final definition has none).
  *   - Sketch matrices G are data, not drawn here: [sets, g_len] with sets = heads when
  *     sketch_per_head != 0, else 1 (the paper shares one phi' per layer, Section 4), and inside
  *     a set the p/2 matrices of shape d x r followed by the p/2 - 2 matrices of shape r x r

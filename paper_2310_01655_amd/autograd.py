@@ -48,12 +48,16 @@ class _CausalPolysketchAttention(torch.autograd.Function):
         return dQ, dK, dV, None, None
 
 
-def causal_polysketch_attention(Q, K, V, G, p, r, b, local=psf.LOCAL_EXACT, per_head=False, learned=False):
+def causal_polysketch_attention(Q, K, V, G, p, r, b, local=psf.LOCAL_EXACT, per_head=False, learned=False, q_norm=None,
+                                k_norm=None):
     """Differentiable causal Polysketch attention (Sections 3, 3.1, 3.2 of the paper) of
     Q, K [batch, heads, n, d] and V [batch, heads, n, dv] on the GPU; G as for
     psf_causal_attn_fwd ([1 or heads, g_len(d, r, p)], None for p = 2; with learned = True the
     networks' parameters of Algorithm 2, [1 or heads, learned_len(d, r, p)]).  Gradients flow to
-    Q, K and V, and to G when it holds learned parameters that require a gradient."""
+    Q, K and V, and to G when it holds learned parameters that require a gradient.  q_norm, k_norm: (weight, bias or None)
+    of a layer normalisation of the query or key rows before the attention (Section 2.1), whose parameters get
+    gradients too."""
+    Q, K = _normed(Q, q_norm), _normed(K, k_norm)
     B, H, n, d = Q.shape
     dtype = {torch.float32: "f32", torch.bfloat16: "bf16"}[Q.dtype]
     desc = psf.make_desc(B, H, n, d, p, r, b, dtype, dv=V.shape[-1], local=local, per_head=per_head,
@@ -109,13 +113,20 @@ class _CausalWindowAttention(torch.autograd.Function):
         return dQ, dK, dV, None, None
 
 
-def causal_window_attention(Q, K, V, window=None, sinks=0, lengths=None, scale=None, tokens_first=False):
+def _normed(x, norm):
+    return x if norm is None else layer_norm(x, *norm)
+
+
+def causal_window_attention(Q, K, V, window=None, sinks=0, lengths=None, scale=None, tokens_first=False, q_norm=None,
+                            k_norm=None):
     """Differentiable softmax attention in which row i sees its last `window` tokens (None: all) and the first `sinks`
     tokens of the sequence.  Q [batch, heads, n, d], K and V [batch, kv_heads, n, d], heads a multiple of kv_heads,
     or with tokens_first all of them [batch, n, heads, d]; d a multiple of 8, at most 128.  lengths: int32 [batch] on the
-    GPU, tokens of each sequence (rows behind them give zeros and get zero gradients)."""
+    GPU, tokens of each sequence (rows behind them give zeros and get zero gradients).  q_norm, k_norm as for
+    causal_polysketch_attention."""
     if Q.dim() != 4 or K.dim() != 4:
         raise ValueError("Q, K, V must have four axes")
+    Q, K = _normed(Q, q_norm), _normed(K, k_norm)
     at = 2 if tokens_first else 1
     dtype = {torch.float32: "f32", torch.bfloat16: "bf16"}[Q.dtype]
     desc = psf.make_window_desc(Q.shape[0], Q.shape[at], Q.shape[3 - at], Q.shape[3], window, sinks, dtype,

@@ -184,3 +184,30 @@ def test_gradient_against_differences():
         by_difference, by_gradient = (value[0] - value[1]) / (2 * step), (got[name].double() * way.double()).sum()
         # third derivatives (step^2 / 6 of slopes of order one) and 240 roundings of 2^-24 over the step
         assert abs(by_difference - by_gradient) < 1e-2 * got[name].double().norm() + 240 * 2.0 ** -24 * 4 / step
+
+
+def test_inside_the_attention_layers():
+    """q_norm and k_norm are the normalisation before the call, with gradients of their parameters."""
+    g = torch.Generator().manual_seed(10)
+    Q, K, V, dO = (torch.randn(2, 2, 256, 64, generator=g).cuda().requires_grad_(True) for _ in range(4))
+    G = torch.randn(1, psf.g_len(64, 16, 4), generator=g).cuda()
+    norms = [(1 + 0.1 * torch.randn(64, generator=g)).cuda().requires_grad_(True) for _ in range(3)]
+    q_norm, k_norm = (norms[0], norms[1]), (norms[2],)
+    for layer in (lambda q, k, **more: autograd.causal_polysketch_attention(q, k, V, G, 4, 16, 64, **more),
+                  lambda q, k, **more: autograd.causal_window_attention(q, k, V, 50, 3, **more)):
+        inside = layer(Q, K, q_norm=q_norm, k_norm=k_norm)
+        before = layer(autograd.layer_norm(Q, *q_norm), autograd.layer_norm(K, *k_norm))
+        assert torch.equal(inside, before)
+        for a, c in zip(torch.autograd.grad(inside, [Q, K, V] + norms, dO), torch.autograd.grad(before, [Q, K, V] + norms, dO)):
+            assert torch.equal(a, c) and torch.isfinite(a).all() and a.any()
+
+
+def test_second_derivatives_are_refused():
+    x, w, b, dy = make(10, 64, "f32", seed=11)
+    x.requires_grad_(True)
+    y = autograd.layer_norm(x, w, b)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(y, x, dy, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        heads = x.view(1, 1, 10, 64)
+        torch.autograd.grad(autograd.causal_window_attention(heads, heads, heads), x, dy.view(1, 1, 10, 64), create_graph=True)
