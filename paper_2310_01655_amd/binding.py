@@ -613,43 +613,58 @@ def _done(st, where):
 
 
 def _norm_rows(x):
-    if x.dim() == 0 or x.dtype not in _CODES:
+    """(rows, width, type code) of a tensor of rows."""
+    code, shape = _CODES.get(x.dtype), x.shape
+    if code is None or not shape:
         raise ValueError("x must be a float32 or bfloat16 tensor of rows")
-    width = x.shape[-1]
-    return (x.numel() // width if width else 0), width
+    width = shape[-1]
+    return (x.numel() // width if width else 0), width, code
+
+
+@functools.lru_cache(maxsize=64)
+def _norm_bwd_bytes(rows, width, code):
+    return lib().psf_layer_norm_bwd_workspace_bytes(rows, width, code)
 
 
 def psf_layer_norm_fwd(x, weight, bias=None, eps=1e-6, y=None, stats=None, want_stats=False, stream=None):
     """Layer normalisation over the last axis; returns y, or (y, stats) with want_stats or a stats tensor ([rows, 2]
     fp32: mean and inverse deviation, for psf_layer_norm_bwd)."""
-    rows, width = _norm_rows(x)
+    rows, width, code = _norm_rows(x)
     where, device = _place(stream, x, weight, bias, y, stats)
+    dtype = x.dtype
+    x_ptr = _ptr(x, dtype, None, "x")
     with where:
         if y is None:
-            y = torch.empty_like(x, memory_format=torch.contiguous_format)
+            y = torch.empty_like(x)
         if stats is None and want_stats:
-            stats = torch.empty(rows, 2, dtype=torch.float32, device=device)
-        _done(lib().psf_layer_norm_fwd(rows, width, _CODES[x.dtype], eps, _ptr(x, x.dtype, None, "x"),
-                                       _ptr(weight, x.dtype, (width,), "weight"), _ptr(bias, x.dtype, (width,), "bias"),
-                                       _ptr(y, x.dtype, x.shape, "y"), _ptr(stats, torch.float32, (rows, 2), "stats"),
-                                       _stream_ptr(None)), "psf_layer_norm_fwd")
+            stats = torch.empty((rows, 2), dtype=torch.float32, device=device)
+        st = lib().psf_layer_norm_fwd(rows, width, code, eps, x_ptr, _ptr(weight, dtype, (width,), "weight"),
+                                      _ptr(bias, dtype, (width,), "bias"), _ptr(y, dtype, x.shape, "y"),
+                                      _ptr(stats, torch.float32, (rows, 2), "stats"), _stream_ptr(None))
+    if st != PSF_OK:
+        raise PsfError(st, "psf_layer_norm_fwd")
     return y if stats is None else (y, stats)
 
 
 def psf_layer_norm_bwd(x, weight, stats, dy, want_bias=True, workspace=None, stream=None):
     """Gradients of psf_layer_norm_fwd: (dx, dweight, dbias), dbias None without want_bias."""
-    rows, width = _norm_rows(x)
+    rows, width, code = _norm_rows(x)
     where, device = _place(stream, x, weight, stats, dy)
+    dtype = x.dtype
+    x_ptr, weight_ptr = _ptr(x, dtype, None, "x"), _ptr(weight, dtype, (width,), "weight")
     with where:
-        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
-        dweight = torch.empty_like(weight)
+        dx, dweight = torch.empty_like(x), torch.empty_like(weight)
         dbias = torch.empty_like(weight) if want_bias else None
-        code = _CODES[x.dtype]
-        workspace = _room(workspace, lambda: lib().psf_layer_norm_bwd_workspace_bytes(rows, width, code), device)
-        _done(lib().psf_layer_norm_bwd(rows, width, code, _ptr(x, x.dtype, None, "x"), _ptr(weight, x.dtype, (width,), "weight"),
-                                       _ptr(stats, torch.float32, (rows, 2), "stats"), _ptr(dy, x.dtype, x.shape, "dy"),
-                                       dx.data_ptr(), dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
-                                       *_room_args(workspace), _stream_ptr(None)), "psf_layer_norm_bwd")
+        if workspace is None:
+            workspace = torch.empty(_norm_bwd_bytes(rows, width, code), dtype=torch.uint8, device=device)
+        else:
+            workspace = _room(workspace, None, device)
+        st = lib().psf_layer_norm_bwd(rows, width, code, x_ptr, weight_ptr, _ptr(stats, torch.float32, (rows, 2), "stats"),
+                                      _ptr(dy, dtype, x.shape, "dy"), dx.data_ptr(), dweight.data_ptr(),
+                                      None if dbias is None else dbias.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                      _stream_ptr(None))
+    if st != PSF_OK:
+        raise PsfError(st, "psf_layer_norm_bwd")
     return dx, dweight, dbias
 
 
