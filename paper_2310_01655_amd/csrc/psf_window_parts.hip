@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256) void window_parts_fwd_kernel(const S *Q, const
 
 // dQ: as forward, a wave owns 16 queries; and D = <dO, o> of every row for the kernel below.
 template <int NT, typename S>
-__global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const S *K, const S *V, const S *O, const S *dO,
+__global__ __launch_bounds__(256, 2) void window_parts_dq_kernel(const S *Q, const S *K, const S *V, const S *O, const S *dO,
                                                               const int32_t *lengths, const float *lse, float *delta, S *dQ,
                                                               Window w)
 {
@@ -204,9 +204,11 @@ __global__ __launch_bounds__(256) void window_parts_dq_kernel(const S *Q, const 
     for (int t = 0; t < NT; ++t) store_piece(dQ + at_q + i * w.row_q, 16 * t + 4 * g, d, 1, acc[t] * w.scale);
 }
 
-// dK, dV: a wave owns 16 keys, tiles of 32 queries pass, head after head of the group.
+// dK, dV: a wave owns 16 keys, tiles of 32 queries pass, head after head of the group.  Two waves a SIMD where the sums of d = 64
+// leave the room (2 x 12 x 1951, window 300, both kernels: 155 us instead of 168); at d = 128 they would not stay in registers
+// (2 x 8 x 2000, window 500: 335 instead of 293).
 template <int NT, typename S>
-__global__ __launch_bounds__(256) void window_parts_dkv_kernel(const S *Q, const S *K, const S *V, const S *dO,
+__global__ __launch_bounds__(256, NT == 4 ? 2 : 1) void window_parts_dkv_kernel(const S *Q, const S *K, const S *V, const S *dO,
                                                                const int32_t *lengths, const float *lse, const float *delta,
                                                                S *dK, S *dV, float *room, Window w, KeyWalks walks)
 {
