@@ -387,7 +387,7 @@ typedef struct {
     int32_t window, sinks;   /* window >= 1, sinks >= 0                                               */
     int32_t dtype;           /* psf_dtype of every tensor                                             */
     int32_t layout;          /* psf_layout of every tensor                                            */
-    float scale;             /* of the scores, 1 / sqrt(d) as a rule                                  */
+    float scale;             /* of the scores, finite; 1 / sqrt(d) as a rule                          */
 } psf_window_desc;
 psf_status psf_check_window_desc(const psf_window_desc *desc);
 
@@ -400,7 +400,7 @@ psf_status psf_check_window_desc(const psf_window_desc *desc);
  * An infinity or NaN of a token reaches no row that does not see the token.
  *
  * psf_window_attn_bwd -- gradients of L(O) for a given dO: dQ, dK, dV in the layout of Q, K, V, each written once
- * (zero behind the lengths); O and lse as the forward call wrote them.  dK and dV are summed over the query
+ * (zero behind the lengths; no alias of any input); O and lse as the forward call wrote them.  dK and dV are summed over the query
  * heads that share the key head.  No atomics: a repeated call returns the same bits.  In bf16 storage
  * weights and their gradients are rounded to bf16 for their products.  An infinity or NaN reaches no gradient of a
  * token with which it shares no visible pair.
@@ -443,9 +443,9 @@ psf_status psf_cache_append(const psf_cache_desc *desc, int32_t n, const void *K
                             const int32_t *table, const int32_t *lengths, const int32_t *counts, void *hip_stream);
 
 /*
- * psf_cache_fork -- for k < forks: sequence children[k] becomes what parents[k] is.  It shares the parent's pages, but
- * for a last page that is not full, whose content is copied to page fresh[k] (not read otherwise); row children[k] of
- * the table and lengths[children[k]] are overwritten.  A parent of several children is fine; a child that is
+ * psf_cache_fork -- for k < forks (1 to 65535): sequence children[k] becomes what parents[k] is.  It shares the parent's
+ * pages, but for a last page that is not full, whose content is copied to page fresh[k] (not used where there is no such
+ * page; where fresh[k] is none, neither has the child one); row children[k] of the table and lengths[children[k]] are overwritten.  A parent of several children is fine; a child that is
  * also a parent in the same call, or named twice, gets unspecified content.  Pairs with a sequence outside
  * [0, seqs), or with parent == child, are left out.
  */

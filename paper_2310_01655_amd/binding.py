@@ -764,8 +764,10 @@ def psf_cache_append(desc, K, V, Kp, Vp, table, lengths, counts=None, stream=Non
 
 def psf_cache_fork(desc, Kp, Vp, table, lengths, parents, children, fresh, stream=None):
     """Sequence children[k] becomes a copy of parents[k] that shares its full pages; a last page that is not full is copied
-    to page fresh[k].  Writes the children's rows of table and lengths."""
+    to page fresh[k].  Writes the children's rows of table and lengths.  No forks: nothing is done."""
     forks = (parents.numel(),)
+    if forks[0] == 0:
+        return
     where, _ = _place(stream, Kp, Vp, table, lengths, parents, children, fresh)
     with where:
         _done(lib().psf_cache_fork(ctypes.byref(desc), forks[0], *_cache_ptrs(desc, Kp, Vp, table, lengths),

@@ -102,11 +102,11 @@ __global__ __launch_bounds__(kCacheThreads) void cache_fork_kernel(u4 *Kp, u4 *V
     const int length = lengths[parent], last = length > 0 ? length / c.page : 0;
     const bool part = length > 0 && length % c.page != 0 && last < c.cols;
     const int own = (unsigned)fresh[k] < (unsigned)c.pages ? fresh[k] : -1;
+    const int old = part ? page_of(from, last, c.cols, c.pages) : -1;      // (no page there: the child has none either)
     if (blockIdx.x == 0) {
-        for (int i = threadIdx.x; i < c.cols; i += kCacheThreads) to[i] = part && i == last ? own : from[i];
+        for (int i = threadIdx.x; i < c.cols; i += kCacheThreads) to[i] = old >= 0 && i == last ? own : from[i];
         if (threadIdx.x == 0) lengths[child] = length;
     }
-    const int old = part ? page_of(from, last, c.cols, c.pages) : -1;
     if (old >= 0 && own >= 0) copy_page(Kp, Vp, pieces, old, own, blockIdx.x, gridDim.x);
 }
 

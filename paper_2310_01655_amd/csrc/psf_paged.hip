@@ -365,6 +365,7 @@ psf_status psf_paged_attn(const psf_cache_desc *desc, int32_t heads, int32_t win
     const psf_status st = check(desc, heads, &sh.c);
     if (st != PSF_OK) return st;
     if (window <= 0 || sinks < 0) return PSF_ERR_SHAPE;
+    if (!(fabsf(scale) < INFINITY)) return PSF_ERR_UNSUPPORTED;
     if (!q || !Kp || !Vp || !table || !lengths || !o) return PSF_ERR_NULL;
     const size_t need = psf_paged_workspace_bytes(desc, heads);
     if (need > 0 && !workspace) return PSF_ERR_NULL;

@@ -226,6 +226,18 @@ def test_fork(dtype, page, kv, d):
     assert same(Kp.cpu(), want_k) and torch.equal(table[:8].cpu(), rows[:8]) and n[8] == 1 and table[8, 0] == -1
 
 
+def test_fork_of_a_sequence_with_freed_pages():
+    """A parent whose last page has been freed: its child has none there either, and the fresh page stays as it is."""
+    desc, Kp, Vp, table, n, free = make_cache([40, 40, 0, 0], 16, 2, 64, "bf16", spare=4)
+    table[0, 2], table[1, 1] = -1, -1
+    before, rows = Kp.clone(), table.clone()
+    psf.psf_cache_fork(desc, Kp, Vp, table, n, ints([0, 1]), ints([2, 3]), ints(free[:2]))
+    assert torch.equal(table[2], rows[0]) and n.tolist() == [40] * 4
+    assert table[3].tolist() == rows[1, :2].tolist() + [free[1]] + rows[1, 3:].tolist()
+    assert same(Kp[free[0]], before[free[0]]) and same(Kp[free[1]], before[int(rows[1, 2])])
+    psf.psf_cache_fork(desc, Kp, Vp, table, n, *(torch.empty(0, dtype=torch.int32, device="cuda") for _ in range(3)))
+
+
 def model_compact(Kp, Vp, table, lengths, page):
     pages, rows = Kp.shape[0], table.tolist()
     used = [row[:max(0, -(-n // page))] for row, n in zip(rows, lengths)]

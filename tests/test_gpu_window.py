@@ -79,8 +79,9 @@ def test_unequal_lengths(shape, lengths, dtype, tokens_first):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_tokens_first_and_scale(dtype):
     Q, K, V, dO = make(2, 6, 2, 210, 64, dtype, seed=2)
-    got, _ = run(Q, K, V, dO, 77, 5, scale=0.3, tokens_first=True)
-    check(got, window_reference(Q, K, V, 77, 5, scale=0.3, dO=dO), "tokens first")
+    for scale in (0.3, -0.2, 0.0):
+        got, _ = run(Q, K, V, dO, 77, 5, scale=scale, tokens_first=True)
+        check(got, window_reference(Q, K, V, 77, 5, scale=scale, dO=dO), "tokens first, scale %g" % scale)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

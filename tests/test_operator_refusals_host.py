@@ -26,6 +26,8 @@ WINDOW = psf.make_window_desc(2, 8, 1000, 64, 100, 4, kv_heads=2)
     ({}, OK), (dict(batch=0), SHAPE), (dict(heads=-1), SHAPE), (dict(kv_heads=3), SHAPE), (dict(kv_heads=0), SHAPE), (dict(n=0), SHAPE),
     (dict(d=0), SHAPE), (dict(window=0), SHAPE), (dict(sinks=-1), SHAPE), (dict(dtype=2), UNSUPPORTED), (dict(layout=2), UNSUPPORTED),
     (dict(d=60), UNSUPPORTED), (dict(d=136), UNSUPPORTED), (dict(n=(1 << 24) + 1), UNSUPPORTED), (dict(batch=65536), UNSUPPORTED),
+    (dict(scale=float("inf")), UNSUPPORTED), (dict(scale=float("nan")), UNSUPPORTED), (dict(scale=-0.5), OK),
+    (dict(batch=8, heads=8192, kv_heads=1, n=1 << 16, d=8), UNSUPPORTED), (dict(heads=16384, kv_heads=1, d=128), UNSUPPORTED),
     (dict(window=2 ** 31 - 1), OK), (dict(sinks=2 ** 31 - 1), OK), (dict(d=128, n=1), OK),
 ])
 def test_window_descriptor(fields, code):
@@ -130,6 +132,8 @@ def test_paged_attention_sizes():
     call = lambda heads=8, window=1, sinks=0, args=(P,) * 7, room=need: L.psf_paged_attn(ref, heads, window, sinks, 1.0, *args, room, None)
     assert call(heads=6) == SHAPE and call(heads=0) == SHAPE and call(window=0) == SHAPE and call(sinks=-1) == SHAPE
     assert call(heads=4 << 20) == UNSUPPORTED
+    for scale in (float("inf"), float("nan")):
+        assert L.psf_paged_attn(ref, 8, 1, 0, scale, *[P] * 7, need, None) == UNSUPPORTED
     for k in range(7):
         assert call(args=[None if i == k else P for i in range(7)]) == NULL
     for k in (0, 1, 2, 5):

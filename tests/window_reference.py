@@ -4,12 +4,12 @@
 The bounds follow the arithmetic of a correct implementation on the stored inputs; u is half a step of the storage
 type relative to a value (bf16 2^-8, fp32 2^-24), r the rounding of a weight for its product (2^-8 in bf16
 storage, 2^-22 for fp32 from three parts), all first order with a few per cent on top:
-  score     |error| <= ds = scale (d + 8) 2^-23 sum_c |q_c k_c|       (fp32 products and sums)
+  score     |error| <= ds = |scale| (d + 8) 2^-23 sum_c |q_c k_c|       (fp32 products and sums)
   weight    relative error E <= 2 max_j ds + (4 + max |s|) 2^-21      (exponent, maximum, sum, L)
   o         sum_j p (r + E + (n + 8) 2^-24) |v| + u |o|
   D         sum_c |dO_c| (error of the stored o_c + (d + 8) 2^-24 |o_c|)
   dS        p (r |t| + E |t| + eD + e_t),  t = <dO, v> - D,  e_t = (d + 8) 2^-23 sum_c |dO_c v_c|
-  dQ, dK    scale sum (error of dS + (n + 8) 2^-24 |dS|) |k or q| + u |result|
+  dQ, dK    |scale| sum (error of dS + (n + 8) 2^-24 |dS|) |k or q| + u |result|
   dV        sum_i p (r + E + (n + 8) 2^-24) |dO| + u |dV|
 """
 import torch
@@ -42,7 +42,7 @@ def window_reference(Q, K, V, window, sinks, lengths=None, scale=None, dO=None):
             q, k, v = Q[b, h, :end].double(), K[b, kv, :end].double(), V[b, kv, :end].double()
             s = torch.where(seen, scale * (q @ k.T), float("-inf"))
             p = torch.softmax(s, 1)
-            ds = torch.where(seen, scale * (d + 8) * 2.0 ** -23 * (q.abs() @ k.abs().T), 0.0)
+            ds = torch.where(seen, abs(scale) * (d + 8) * 2.0 ** -23 * (q.abs() @ k.abs().T), 0.0)
             E = 2 * ds.amax(1, keepdim=True) + (4 + torch.where(seen, s.abs(), 0.0).amax(1, keepdim=True)) * 2.0 ** -21
             o = p @ v
             bound = (p * (r + E + sums)) @ v.abs() + u * o.abs()
@@ -57,9 +57,9 @@ def window_reference(Q, K, V, window, sinks, lengths=None, scale=None, dO=None):
             dS = p * t
             eS = p * ((r + E) * t.abs() + eD + et) + sums * dS.abs()
             out["dQ"][0][b, h, :end] = scale * (dS @ k)
-            out["dQ"][1][b, h, :end] = scale * (eS @ k.abs())
+            out["dQ"][1][b, h, :end] = abs(scale) * (eS @ k.abs())
             out["dK"][0][b, kv, :end] += scale * (dS.T @ q)
-            out["dK"][1][b, kv, :end] += scale * (eS.T @ q.abs())
+            out["dK"][1][b, kv, :end] += abs(scale) * (eS.T @ q.abs())
             out["dV"][0][b, kv, :end] += p.T @ g
             out["dV"][1][b, kv, :end] += (p * (r + E + sums)).T @ g.abs()
     for x in names[1:]:
