@@ -561,27 +561,27 @@ _AS_IT_IS = contextlib.nullcontext()
 def _place(stream, *tensors):
     """(context, device) of a call on these GPU tensors: with the context the device is the current one and `stream`
     the current stream."""
-    device = None
+    first = tensors[0]
+    index = first.get_device()
     for t in tensors:
-        if t is None:
-            continue
-        if device is None:
-            if not t.is_cuda:
-                raise ValueError("tensors must live on the GPU (no CPU path exists)")
-            device = t.device
-        elif t.device != device:
-            raise ValueError("all tensors of a call must live on one GPU, not on %s and %s" % (device, t.device))
+        if t is not None and t.get_device() != index:
+            raise ValueError("all tensors of a call must live on one GPU, not on %s and %s" % (first.device, t.device))
+    if index < 0:
+        raise ValueError("tensors must live on the GPU (no CPU path exists)")
     if stream is not None:
-        if stream.device != device:
-            raise ValueError("the stream belongs to %s, the tensors live on %s" % (stream.device, device))
-        return torch.cuda.stream(stream), device
-    return (_AS_IT_IS if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)), device
+        if stream.device != first.device:
+            raise ValueError("the stream belongs to %s, the tensors live on %s" % (stream.device, first.device))
+        return torch.cuda.stream(stream), first.device
+    if index != torch._C._cuda_getDevice():
+        return torch.cuda.device(index), first.device
+    return _AS_IT_IS, first.device
 
 
 def _ptr(t, dtype, shape, name):
     """Address of a contiguous tensor of this type and shape (None: no tensor)."""
     if t is None:
         return None
+    # (the common case in one condition, as in _dev_ptr)
     if t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape):
         return t.data_ptr()
     if t.dtype is not dtype:

@@ -15,7 +15,7 @@ namespace psf {
 namespace {
 
 constexpr int kPagedStep = 32;             // positions a wave takes at a time
-constexpr int kPagedWaves = 4;
+constexpr int kPagedWaves = 4, kPagedMany = 8;   // waves of a workgroup, and of one that has a short sequence to itself
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct PagedShape {
@@ -124,8 +124,8 @@ struct Steps {
 
 // (At least two waves a SIMD: fp32 rows of 128 leave to itself at one, 90 us for 16 contexts of 5000 tokens and four key heads
 // instead of 74; bf16 rows reach three.)
-template <typename T, int DP>
-__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attn_kernel(const T *q, const T *Kp, const T *Vp, const int32_t *table,
+template <typename T, int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_attn_kernel(const T *q, const T *Kp, const T *Vp, const int32_t *table,
                                                                       const int32_t *lengths, T *o, float *sums, float *parts,
                                                                       PagedShape sh)
 {
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attn_kernel(const T
         return p < 0 ? -1 : (p * sh.c.kv_heads + kv) * sh.c.page + (int)slot;
     };
     int next = begin + wave < end ? row_at(steps.at(begin + wave)) : -1;
-    for (int k = begin + wave; k < end; k += kPagedWaves) {
+    for (int k = begin + wave; k < end; k += WAVES) {
         const int mine = next;
         Eight<T> key[2][KS];
         Values<T, VW> val[8];
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attn_kernel(const T
             val[e].zero();
             if (rows[e] >= 0 && VW * li < d) val[e].load(Vp + (size_t)rows[e] * d + VW * li);
         }
-        if (k + kPagedWaves < end) next = row_at(steps.at(k + kPagedWaves));
+        if (k + WAVES < end) next = row_at(steps.at(k + WAVES));
         float w[8];
         float most = -INFINITY;
 #pragma unroll
@@ -214,16 +214,22 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attn_kernel(const T
         settle_parts();                                    // the sums are read at the next step's head
     }
 
-    // the four waves together
-    __shared__ float tops[kPagedWaves][16], totals[kPagedWaves][16];
-    __shared__ float lds[kPagedWaves][16][DP + 4];
+    // the waves together
+    __shared__ float tops[WAVES][16], totals[WAVES][16];
+    __shared__ float lds[WAVES][16][DP + 4];
     sum = over_groups(sum);
     if (g == 0) {
         tops[wave][li] = top;
         totals[wave][li] = sum;
     }
     __syncthreads();
-    float all = fmaxf(fmaxf(tops[0][li], tops[1][li]), fmaxf(tops[2][li], tops[3][li]));
+    auto highest = [&](int h) {
+        float most = tops[0][h];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) most = fmaxf(most, tops[w][h]);
+        return most;
+    };
+    float all = highest(li);
     const float share = top == -INFINITY ? 0.f : exp2f(top - all);
 #pragma unroll
     for (int j = 0; j < VW; ++j)
@@ -231,17 +237,21 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attn_kernel(const T
         for (int e = 0; e < 4; ++e) lds[wave][li][VW * (4 * g + e) + j] = acc[j][e] * share;
     __syncthreads();
     const int h = threadIdx.x / 16, c = threadIdx.x % 16;  // 256 threads: 16 heads, VW columns each
-    if (16 * tile + h >= sh.group || VW * c >= d) return;
-    all = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h]));
+    if (h >= 16 || 16 * tile + h >= sh.group || VW * c >= d) return;
+    all = highest(h);
     float total = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) total += tops[w][h] == -INFINITY ? 0.f : totals[w][h] * exp2f(tops[w][h] - all);
+    for (int w = 0; w < WAVES; ++w) total += tops[w][h] == -INFINITY ? 0.f : totals[w][h] * exp2f(tops[w][h] - all);
     const size_t row = (size_t)seq * sh.heads + kv * sh.group + 16 * tile + h;
     const float by = sh.splits > 1 ? 1.f : total > 0.f || total != total ? 1.f / total : 0.f;
     float out[VW];
 #pragma unroll
-    for (int j = 0; j < VW; ++j) out[j] = ((lds[0][h][VW * c + j] + lds[1][h][VW * c + j]) +
-                                           (lds[2][h][VW * c + j] + lds[3][h][VW * c + j])) * by;
+    for (int j = 0; j < VW; ++j) {
+        out[j] = lds[0][h][VW * c + j];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) out[j] += lds[w][h][VW * c + j];
+        out[j] *= by;
+    }
     if (sh.splits == 1) {
 #pragma unroll
         for (int j = 0; j < VW; j += 4) store4(o + row * d + VW * c + j, f4{out[j], out[j + 1], out[j + 2], out[j + 3]});
@@ -302,13 +312,27 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const float *s
     }
 }
 
+long long paged_units(const Cache &c, int heads) { return (long long)c.seqs * c.kv_heads * ((heads / c.kv_heads + 15) / 16); }
+
+// Where a table holds short sequences only, a workgroup of kPagedMany waves has one to itself, which saves the second launch:
+// up to 4 steps a wave, one in fp32 (its products take four times as long), four times that where there are as
+// many workgroups as CUs.  Without the split and with it, us: one sequence, 12 key heads of 64, bf16, 1000 tokens 11.3 and
+// 13.6, 1500 14.7 and 13.4; 64 such sequences, 500 20.0 and 22.6, 4000 138 and 143; fp32, 4 key heads of 128, one sequence of
+// 100 11.0 and 13.2, of 500 20 and 13.4; 64 of 500 27 and 32.
+bool paged_short(const Cache &c, int heads)
+{
+    const int steps = (c.bf16 ? 4 : 1) * (paged_units(c, heads) >= 256 ? 4 : 1);
+    return (long long)c.cols * c.page <= steps * kPagedMany * kPagedStep;
+}
+
 // Workgroups that share a sequence's positions: as many as make 1024 workgroups of the whole call (four a CU), but
 // no fewer than 128 positions (a step for every wave) of the longest sequence the table can hold.  Measured with 512, 768,
 // 1024 and 1536 (us): 64 contexts of 300 to 12000 tokens 179, 180, 166, 160; three of 100000 70, 67, 68, 74; 16 of 2500
 // 32, 34, 33, 35; 64 behind a window of 1024 31, 32, 34, 34.
 int paged_splits(const Cache &c, int heads)
 {
-    const long long units = (long long)c.seqs * c.kv_heads * ((heads / c.kv_heads + 15) / 16);
+    if (paged_short(c, heads)) return 1;
+    const long long units = paged_units(c, heads);
     const long long steps = ((long long)c.cols * c.page + kPagedWaves * kPagedStep - 1) / (kPagedWaves * kPagedStep);
     long long splits = (1024 + units - 1) / units;
     if (splits > steps) splits = steps;
@@ -331,8 +355,13 @@ psf_status launch(const void *q, const void *Kp, const void *Vp, const int32_t *
     const size_t rows = (size_t)sh.c.seqs * sh.heads;
     float *sums = (float *)ws, *parts = sums ? sums + align_up(2 * rows * sh.splits, 64) : nullptr;
     const uint32_t groups = (uint32_t)sh.c.seqs * sh.c.kv_heads * sh.head_tiles * sh.splits;
-    hipLaunchKernelGGL((paged_attn_kernel<T, DP>), dim3(groups), dim3(64 * kPagedWaves), 0, s, (const T *)q, (const T *)Kp,
-                       (const T *)Vp, table, lengths, (T *)o, sums, parts, sh);
+    auto go = [&](auto waves) {
+        constexpr int WAVES = decltype(waves)::value;
+        hipLaunchKernelGGL((paged_attn_kernel<T, DP, WAVES>), dim3(groups), dim3(64 * WAVES), 0, s, (const T *)q, (const T *)Kp,
+                           (const T *)Vp, table, lengths, (T *)o, sums, parts, sh);
+    };
+    if (paged_short(sh.c, sh.heads)) go(std::integral_constant<int, kPagedMany>{});
+    else go(std::integral_constant<int, kPagedWaves>{});
     PSF_LAUNCH_CHECK();
     if (sh.splits == 1) return PSF_OK;
     hipLaunchKernelGGL((paged_join_kernel<T, DP>), dim3((uint32_t)rows), dim3(kJoinThreads), 0, s, sums, parts, (T *)o, (int)rows, sh.c.d,

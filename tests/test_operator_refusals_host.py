@@ -85,7 +85,7 @@ def test_layer_norm_pointers():
     assert L.psf_layer_norm_bwd(5, 64, 1, *[P] * 6, P + 1, P, need, None) == ALIGNMENT
 
 
-CACHE = psf.make_cache_desc(100, 16, 4, 64, 8, 20)
+CACHE = psf.make_cache_desc(100, 16, 4, 64, 8, 200)
 
 
 @pytest.mark.parametrize("fields,code", [
