@@ -396,14 +396,14 @@ psf_status psf_check_window_desc(const psf_window_desc *desc);
  * lengths[b] tokens (taken as 0 below 0, as n above n); rows behind them are not read, their
  * results are zero.  lse: fp32 [batch, heads, n] (device), log of the sum of exponentials of every row for
  * the backward call (-inf behind the length); NULL to skip it.  Tensors 16-byte aligned (PSF_ERR_ALIGNMENT).
- * Sums are fp32; in bf16 storage the weights are rounded to bf16 for their product with V.
+ * Sums are fp32; in bf16 storage the weights are rounded to bf16 for their product with V (in calls of more than 32 tokens).
  * An infinity or NaN of a token reaches no row that does not see the token.
  *
  * psf_window_attn_bwd -- gradients of L(O) for a given dO: dQ, dK, dV in the layout of Q, K, V, each written once
  * (zero behind the lengths; no alias of any input); O and lse as the forward call wrote them.  dK and dV are summed over the query
  * heads that share the key head.  No atomics: a repeated call returns the same bits.  In bf16 storage
- * weights and their gradients are rounded to bf16 for their products.  An infinity or NaN reaches no gradient of a
- * token with which it shares no visible pair.
+ * weights and their gradients are rounded to bf16 for their products (in calls of more than 32 tokens).  An infinity
+ * or NaN reaches no gradient of a token with which it shares no visible pair.
  *   workspace: psf_window_attn_bwd_workspace_bytes(desc) bytes, 256-byte aligned.
  * Nothing is allocated and nothing synchronises.
  */

@@ -137,6 +137,7 @@ inline size_t key_walks_room(const Window &w, const KeyWalks &k, int own)
 psf_status window_bf16_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s);
 psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s);
 size_t window_bf16_room(const Window &w);              // bytes of WindowPtrs::room
+psf_status window_bf16_delta(const Window &w, const WindowPtrs &p, bool all, hipStream_t s);   // D of rows of few keys, or of all
 psf_status window_parts_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s);
 psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s);
 size_t window_parts_room(const Window &w);

@@ -21,15 +21,13 @@ constexpr float kLazy = 8.0f;              // a maximum is left as it is until o
 template <int D, int TILE = kTile>
 struct Staged {
     static constexpr int BYTES = TILE * D * 2, COPIES = BYTES / (kThreads * 16), ROWS = kThreads * 8 / D;   // rows a copy
-    uint32_t wave_at, lane_row, lane_piece, step;          // LDS address of the wave's pieces; row, byte offset of the piece
+    uint32_t wave_at, lane_row, lane_piece;                // LDS address of the wave's pieces; row, byte offset of the piece
     __device__ __forceinline__ Staged(const void *lds, int d)
     {
         wave_at = lds_address(lds) + (threadIdx.x >> 6) * 1024;
         lane_row = threadIdx.x / (D / 8);
-        uint32_t piece = threadIdx.x % (D / 8) ^ row_swz<D>((int)lane_row);
-        if (D != 64 || d != 64) piece = piece < (uint32_t)d / 8 ? piece : 0;   // (columns that are not there: any)
-        lane_piece = piece * 16;
-        step = 0;
+        const uint32_t piece = threadIdx.x % (D / 8) ^ row_swz<D>((int)lane_row);
+        lane_piece = (piece < (uint32_t)d / 8 ? piece : 0) * 16;               // (columns that are not there: any)
     }
     // rows j0 .. of x and y (rows of `ld` values; those from `end` on: row end - 1 instead), to buffer `buf`
     __device__ __forceinline__ void copy(const bf16_t *x, const bf16_t *y, int64_t ld, int j0, int end, int buf) const
@@ -428,7 +426,54 @@ __device__ __forceinline__ void dkv_again(const Window &w, const bf16_t *Q, cons
     }
 }
 
-// dQ, and D = <dO, o> of every row for the kernel below.
+// Whether the kernel below forms D of a wave's rows, from row i0 on.  In a row of few keys dS = p (<dO, v> - D) is a small difference:
+// D from the stored o, rounded to bf16, leaves up to 2^-8 of <dO, v> where the formula has 0 (a row of one key).  The
+// error of such an o falls with the root of its keys; from 64 on it is an eighth of dS's own rounding.
+constexpr int kFew = 64;
+__host__ __device__ inline bool few_keys(const Window &w, int i0)
+{
+    return i0 < kFew || (int64_t)w.window + w.sinks <= kFew;
+}
+
+// D_i = sum_j p_ij <dO_i, v_j> / sum_j p_ij of rows of few keys: a wave 32 rows, its tiles of keys (at most four) straight from
+// memory.  Bound by the latency of those loads: 6 us for 96 heads' first rows.
+template <int D>
+__global__ __launch_bounds__(64) void window_delta_kernel(const bf16_t *Q, const bf16_t *K, const bf16_t *V, const int32_t *lengths,
+                                                          const float *lse, const bf16_t *dO, float *delta, Window w, uint32_t groups)
+{
+    constexpr int KS = D / 16;
+    const int x = threadIdx.x & 31, h = threadIdx.x >> 5;
+    const uint32_t unit = blockIdx.x / groups;
+    const int b = unit / w.heads, head = unit - b * w.heads;
+    const int end = window_end(lengths, b, w.n), i0 = (int)(blockIdx.x - unit * groups) * kOwn, i = i0 + x;
+    if (i0 >= end) return;
+    const int safe = i < end ? i : end - 1;
+    const int64_t at_q = b * w.batch_q + head * w.head_q + safe * w.row_q, at_k = b * w.batch_k + head / w.group * w.head_k;
+    const float c = w.scale2 == 0.f ? 1.f : fabsf(w.scale2);
+    bf16x8 own[KS], own_g[KS];
+    own_row<D>(Q + at_q, w.d, h, w.scale2, own);
+    own_row<D>(dO + at_q, w.d, h, 1.f, own_g);
+    const size_t row = ((size_t)b * w.heads + head) * w.n + safe;
+    const float L = lse[row] * kWindowLog2e;
+    float dot = 0.f, sum = 0.f;
+    const KeyTiles tiles(w, i0, i0 + kOwn < end ? i0 + kOwn - 1 : end - 1, 32);
+    for (int k = 0; k < tiles.total; ++k) {
+        const int j0 = tiles.at(k) * 32;
+        const f32x16 s = far_scores<D>(K + at_k, w.row_k, j0, end - 1, w.d, own);
+        const f32x16 u = far_scores<D>(V + at_k, w.row_k, j0, end - 1, w.d, own_g);
+        branch_wait();
+        const uint32_t bits = seen_keys(w, i, j0) >> (4 * h);
+        static_for<16>([&](auto e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[int(e)], c, -L));
+            sum += pick<e>(bits, p, 0u);
+            dot += pick<e>(bits, p * u[int(e)], 0u);
+        });
+    }
+    dot = other_half(dot, false) / other_half(sum, false);
+    if (i < end && h == 0) delta[row] = dot;
+}
+
+// dQ, and D = <dO, o> of every other row for the kernel below.
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q, const bf16_t *K, const bf16_t *V,
                                                                 const int32_t *lengths, const bf16_t *O, const float *lse,
@@ -460,18 +505,20 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(const bf16_t *Q,
         bf16x8 own[KS], own_g[KS];
         own_row<D>(Q + at_q + safe * w.row_q, d, h, w.scale2, own);
         own_row<D>(dO + at_q + safe * w.row_q, d, h, 1.f, own_g);
-        {
+        const size_t row = ((size_t)b * w.heads + head) * w.n + safe;
+        if (few_keys(w, i0)) {
+            dot = delta[row];
+        } else {
             bf16x8 o[KS];
             own_row<D>(O + at_q + safe * w.row_q, d, h, 1.f, o);
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dot += (float)o[s][e] * (float)own_g[s][e];
+            dot = other_half(dot, false);
+            if (i < end && h == 0) delta[row] = dot;
         }
-        dot = other_half(dot, false);
-        const size_t row = ((size_t)b * w.heads + head) * w.n + safe;
         L = lse[row] * kWindowLog2e;
-        if (i < end && h == 0) delta[row] = dot;
         const Reads<D> at(lane);
         const uint32_t lds_at = lds_address(lds);
         for (int k = 0; k < tiles.total; ++k) {
@@ -680,6 +727,19 @@ size_t window_bf16_room(const Window &w)
     return key_walks_room(w, walks_of(w), kOwnWg);
 }
 
+psf_status window_bf16_delta(const Window &w, const WindowPtrs &p, bool all, hipStream_t s)
+{
+    const uint32_t groups = ((all || w.n < kFew ? w.n : kFew) + kOwn - 1) / kOwn;
+    auto go = [&](auto width) -> psf_status {
+        constexpr int D = decltype(width)::value;
+        hipLaunchKernelGGL((window_delta_kernel<D>), dim3(groups * w.batch * w.heads), dim3(64), 0, s, (const bf16_t *)p.Q,
+                           (const bf16_t *)p.K, (const bf16_t *)p.V, p.lengths, p.lse, (const bf16_t *)p.dO, p.delta, w, groups);
+        PSF_LAUNCH_CHECK();
+        return PSF_OK;
+    };
+    return w.d <= 64 ? go(std::integral_constant<int, 64>{}) : go(std::integral_constant<int, 128>{});
+}
+
 psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
 {
     auto go = [&](auto width) -> psf_status {
@@ -688,6 +748,7 @@ psf_status window_bf16_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
                      *dO = (const bf16_t *)p.dO;
         bf16_t *dQ = (bf16_t *)p.dQ, *dK = (bf16_t *)p.dK, *dV = (bf16_t *)p.dV;
         const uint32_t groups = (w.n + kOwnWg - 1) / kOwnWg;
+        if (const psf_status st = window_bf16_delta(w, p, few_keys(w, kFew), s); st != PSF_OK) return st;
         hipLaunchKernelGGL((window_dq_kernel<D>), dim3(groups * w.batch * w.heads), dim3(kThreads), 0, s, Q, K, V, p.lengths, O, p.lse,
                            dO, dQ, p.delta, w, groups);
         PSF_LAUNCH_CHECK();

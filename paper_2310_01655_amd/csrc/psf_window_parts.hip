@@ -1,6 +1,8 @@
-// Window attention in fp32 storage on bf16 parts of its values (psf_parts.h): three parts of every value and weight.  A wave owns 16 rows as the columns of its results; tiles of 32 rows
-// of the other side go through LDS, where they are read along their rows for the scores and
-// transposed for the sums.  Bound by the six products that stand for one fp32 product.
+// Window attention on bf16 parts of its values and weights (psf_parts.h): fp32 storage in three parts, and short
+// calls in bf16 storage, whose values are one part.  A wave owns 16 rows as the columns of its results; tiles of 32 rows of
+// the other side go through LDS, where they are read along their rows for the scores and transposed for the
+// sums.  In fp32 bound by the six products that stand for one fp32 product and by taking the tiles apart, which every
+// workgroup does for itself.
 #include "psf_parts.h"
 #include "psf_window.h"
 
@@ -152,23 +154,30 @@ __global__ __launch_bounds__(256, 2) void window_parts_dq_kernel(const S *Q, con
         Parts<P> own[KS], own_g[KS];
         float D = 0.f;
         {
-            OwnRow<KS, S> row, row_g, row_o;
+            OwnRow<KS, S> row, row_g;
             row.load(Q + at_q + safe * w.row_q, d, 1, g);
             row_g.load(dO + at_q + safe * w.row_q, d, 1, g);
-            row_o.load(O + at_q + safe * w.row_q, d, 1, g);
+            if constexpr (P == 3) {
+                OwnRow<KS, S> row_o;
+                row_o.load(O + at_q + safe * w.row_q, d, 1, g);
+#pragma unroll
+                for (int e = 0; e < 2 * KS; ++e) {
+                    const f4 x = row_g.at(e, d, g), y = row_o.at(e, d, g);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) D += x[k] * y[k];
+                }
+            }
             row.parts(own, d, g);
             row_g.parts(own_g, d, g);
-#pragma unroll
-            for (int e = 0; e < 2 * KS; ++e) {
-                const f4 x = row_g.at(e, d, g), y = row_o.at(e, d, g);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) D += x[k] * y[k];
-            }
         }
-        D = over_groups(D);
         const size_t row = ((size_t)b * w.heads + h) * w.n + safe;
         const float L = lse[row] * kWindowLog2e;
-        if (i < end && g == 0) delta[row] = D;
+        if constexpr (P == 3) {
+            D = over_groups(D);
+            if (i < end && g == 0) delta[row] = D;
+        } else {
+            D = delta[row];                                // (formed from the weights before: o is rounded to bf16)
+        }
         const int last = first + kRows < end ? first + kRows - 1 : end - 1;
         const KeyTiles tiles(w, first, last, kTile);
         Tiles next;
@@ -301,8 +310,7 @@ __global__ __launch_bounds__(256, NT == 4 ? 2 : 1) void window_parts_dkv_kernel(
 }
 
 // The shares of the first tokens' gradients added in order: a thread four columns of a row.
-template <typename S>
-__global__ __launch_bounds__(256) void window_parts_share_kernel(S *dK, S *dV, const float *room, Window w, KeyWalks walks)
+__global__ __launch_bounds__(256) void window_parts_share_kernel(float *dK, float *dV, const float *room, Window w, KeyWalks walks)
 {
     const int pieces = w.d / 4, rows = walks.few * kRows;
     const int at = blockIdx.x * 256 + threadIdx.x, row = at / pieces, c = 4 * (at - row * pieces);
@@ -320,19 +328,21 @@ __global__ __launch_bounds__(256) void window_parts_share_kernel(S *dK, S *dV, c
     store4(dV + to, v);
 }
 
+// go(width, a value of the storage type)
 template <class F>
-psf_status with_width(const Window &w, F &&go)
+psf_status with_kind(const Window &w, F &&go)
 {
-    return w.d <= 64 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 8>{});
+    if (w.bf16) return w.d <= 64 ? go(std::integral_constant<int, 4>{}, bf16_t{}) : go(std::integral_constant<int, 8>{}, bf16_t{});
+    return w.d <= 64 ? go(std::integral_constant<int, 4>{}, 0.f) : go(std::integral_constant<int, 8>{}, 0.f);
 }
 
 }  // namespace
 
 psf_status window_parts_fwd(const Window &w, const WindowPtrs &p, void *O, float *lse, hipStream_t s)
 {
-    return with_width(w, [&](auto nt) -> psf_status {
+    return with_kind(w, [&](auto nt, auto value) -> psf_status {
         constexpr int NT = decltype(nt)::value;
-        typedef float S;
+        typedef decltype(value) S;
         hipLaunchKernelGGL((window_parts_fwd_kernel<NT, S>), dim3((w.n + kRows - 1) / kRows, w.batch * w.heads), dim3(256), 0, s,
                            (const S *)p.Q, (const S *)p.K, (const S *)p.V, p.lengths, (S *)O, lse, w);
         PSF_LAUNCH_CHECK();
@@ -344,10 +354,12 @@ size_t window_parts_room(const Window &w) { return key_walks_room(w, key_walks(w
 
 psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
 {
-    return with_width(w, [&](auto nt) -> psf_status {
+    return with_kind(w, [&](auto nt, auto value) -> psf_status {
         constexpr int NT = decltype(nt)::value;
-        typedef float S;
+        typedef decltype(value) S;
         const unsigned tiles = (w.n + kRows - 1) / kRows;
+        if (w.bf16)
+            if (const psf_status st = window_bf16_delta(w, p, true, s); st != PSF_OK) return st;
         hipLaunchKernelGGL((window_parts_dq_kernel<NT, S>), dim3(tiles, w.batch * w.heads), dim3(256), 0, s, (const S *)p.Q,
                            (const S *)p.K, (const S *)p.V, (const S *)p.O, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dQ, w);
         PSF_LAUNCH_CHECK();
@@ -357,10 +369,12 @@ psf_status window_parts_bwd(const Window &w, const WindowPtrs &p, hipStream_t s)
                            (const S *)p.K, (const S *)p.V, (const S *)p.dO, p.lengths, p.lse, p.delta, (S *)p.dK, (S *)p.dV,
                            p.room, w, walks);
         PSF_LAUNCH_CHECK();
-        if (walks.parts == 1) return PSF_OK;
-        hipLaunchKernelGGL((window_parts_share_kernel<S>), dim3((walks.few * kRows * (w.d / 4) + 255) / 256, units), dim3(256), 0, s,
-                           (S *)p.dK, (S *)p.dV, p.room, w, walks);
-        PSF_LAUNCH_CHECK();
+        if constexpr (std::is_same_v<S, float>) {          // (walks of short calls are whole)
+            if (walks.parts == 1) return PSF_OK;
+            hipLaunchKernelGGL(window_parts_share_kernel, dim3((walks.few * kRows * (w.d / 4) + 255) / 256, units), dim3(256), 0, s,
+                               (S *)p.dK, (S *)p.dV, p.room, w, walks);
+            PSF_LAUNCH_CHECK();
+        }
         return PSF_OK;
     });
 }

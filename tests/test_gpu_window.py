@@ -102,6 +102,35 @@ def test_growing_scores():
     check(got, window_reference(Q, K, V, 320, 0, dO=dO), "growing")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(2, 3, 3, 40, 64), (1, 4, 2, 130, 120), (1, 2, 1, 300, 128)])
+def test_rows_of_one_key_have_no_score_gradient(shape, dtype):
+    """With a window of one token p = 1 and dS = p (<dO, v> - D) = 0, whatever o was rounded to.  What may stay: p is
+    exp2 of a sum of a few fp32 roundings of |L| < 64 (2^-16 relative), and <dO, v> itself of d terms in two orders
+    (2^-16 of the sum of its terms' sizes at d = 128)."""
+    Q, K, V, dO = make(*shape, dtype, seed=11)
+    got, lse = run(Q, K, V, dO, window=1, sinks=0)
+    assert lse.abs().max() < 64
+    wide = lambda t: t.double().repeat_interleave(shape[1] // shape[2], 1) if t.shape[1] != shape[1] else t.double()
+    q, k, v, g = (wide(t) for t in (Q, K, V, dO))
+    left = (g.abs() * v.abs()).sum(-1, keepdim=True) * 2.0 ** -15 / shape[4] ** 0.5
+    assert (got["dQ"].double().abs() <= left * k.abs()).all()
+    most = (left * q.abs()).reshape(shape[0], shape[2], -1, *q.shape[2:]).sum(2)
+    assert (got["dK"].double().abs() <= most).all()
+
+
+@pytest.mark.parametrize("shape,lengths", [
+    ((1, 1, 1, 1, 64, 1, 0), None), ((2, 4, 2, 7, 48, 3, 1), [7, 0]), ((3, 8, 2, 32, 128, 40, 0), [32, 5, 31]), ((1, 2, 1, 31, 8, 2, 4), None),
+])
+def test_short_calls_round_the_results_only(shape, lengths):
+    """Up to 32 tokens in bf16 storage: the bounds of fp32 storage and one rounding of the result (2^-8, half a step)."""
+    Q, K, V, dO = make(*shape[:5], "bf16", seed=12)
+    ends = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    got, _ = run(Q, K, V, dO, *shape[5:], lengths=ends)
+    want = window_reference(*(t.float() for t in (Q, K, V)), *shape[5:], lengths=lengths, dO=dO.float())
+    check(got, {x: (value, bound * (1 + 2.0 ** -8) + 2.0 ** -8 * value.abs()) for x, (value, bound) in want.items()}, "short")
+
+
 def test_lse():
     Q, K, V, dO = make(2, 4, 2, 150, 64, "f32", seed=5)
     _, lse = run(Q, K, V, dO, 40, 3)
@@ -116,10 +145,11 @@ def test_lse():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,at", [(200, 97), (60, 31)])
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
-def test_odd_values_stay_with_the_rows_that_see_them(dtype, d, value):
+def test_odd_values_stay_with_the_rows_that_see_them(dtype, d, value, n, at):
     """A non-finite K, V, Q or dO row changes nothing for tokens that share no visible pair with it."""
-    n, window, sinks, at = 200, 20, 3, 97
+    window, sinks = 20, 3
     Q, K, V, dO = make(1, 2, 2, n, d, dtype, seed=6)
     before, _ = run(Q, K, V, dO, window, sinks)
     rows = torch.arange(n, device="cuda")
